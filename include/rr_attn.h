@@ -12,6 +12,9 @@
  * rr_dense_attn_packed, rr_mask_from_dense (caller-made masks), rr_selection_accuracy (the
  * appendix's precision / recall / F1 diagnostic), rr_sparse_attn_ws / rr_dense_attn_ws (attention with a
  * workspace, for short steps), rr_estimate_static (estimation without a workspace argument).
+ * For serving a model whose prompts went through these: rr_window_attn (its layers with a sliding window), rr_paged_write and
+ * rr_paged_attn (the new tokens against a key-value cache in pages), rr_key_weights and rr_cache_evict (a cache held to a
+ * number of positions by accumulated attention weight).
  *
  * Conventions common to all entry points
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The library allocates
@@ -143,7 +146,7 @@ typedef struct {
                                      query's own stride: only the keys up to the query's position are summed
                                      there (default: the whole stride, whatever the head's offset) */
 
-/* Library version as major*10000 + minor*100 + patch (500 = 0.5.0). */
+/* Library version as major*10000 + minor*100 + patch (600 = 0.6.0). */
 int rr_version(void);
 
 /* Static text for a status code; never NULL. */
@@ -317,6 +320,112 @@ int rr_sparse_attn_ws(const rr_shape* shape, const void* Q, const void* K, const
                       void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 int rr_dense_attn_ws(const rr_shape* shape, const void* Q, const void* K, const void* V, int B, void* O, float* lse,
                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Causal attention with a sliding window and sinks (local layers): O = Softmax(Q K^T / sqrt(d) over the keys that the
+ * query sees) V, where the query at position i sees key j iff j <= i and (j > i - window or j < sinks).
+ *   window     >= 1 positions, the query's own among them; sinks >= 0 positions at the front that stay visible.
+ *   seq_first, B  NULL (B is not used then), or packed sequences as rr_dense_attn_packed takes them, B a multiple of 16 up to
+ *              128: windows end and sinks count at the first position of the query's sequence.  Not with Lq < L: RR_ERR_PARAM.
+ *   lse        optional, as for rr_sparse_attn.
+ *   workspace  NULL, or at least rr_window_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards: steps of at
+ *              most 16 positions and 32 query rows per KV head then share the keys of a KV head out among several workgroups
+ *              and read them once for all its query heads.  rr_window_workspace_bytes() is 0 for every other call.
+ * Any L, d and strides of the conventions above.  bf16 with d = 128 (packed: B = 128) runs on a kernel of its own, which rounds
+ * the probabilities to bf16; steps with a workspace and all other shapes hold nothing in fewer than 32 bits.  An infinite
+ * or NaN value of V that no query of a launch's tile sees does not reach it; one that a query in the same tile sees makes the
+ * channel NaN in that tile's other rows, as zero times infinity does.
+ */
+size_t rr_window_workspace_bytes(const rr_shape* shape, int window, int sinks);
+int rr_window_attn(const rr_shape* shape, const void* Q, const void* K, const void* V, int window, int sinks,
+                   const int32_t* seq_first, int B, void* O, float* lse, void* workspace, size_t workspace_bytes,
+                   void* hip_stream);
+
+/*
+ * A key-value cache in pages.  A page holds `page` consecutive positions of one sequence for all KV heads; position p of
+ * sequence b lies in page table[b][p / page] at slot p % page.  K and V are pools of pages addressed as
+ * base + page*kv_stride_b + h*kv_stride_h + slot*kv_stride_l + c with the strides of the rr_shape of the call (so both
+ * [pages, Hkv, page, d] and [pages, page, Hkv, d] are possible).
+ *   weight     [num_pages, Hkv, page] fp32 contiguous: what every position's key has got of softmax weights so far.  May be NULL
+ *              where nothing reads or writes it.
+ *   table      [batch, width] int32.  An entry outside [0, num_pages) is no page: its positions hold nothing, are attended by
+ *              nobody and are not written.
+ *   length     [batch] int32: positions of every sequence, those of the present step among them; held to 0 .. L of the call.
+ *   page       a multiple of 16.
+ * The rr_shape of a call on a cache: batch, Hq, Hkv, d, dtype as ever; L = the most positions that any sequence may have (it
+ * sets the size of the launch and of the workspace: width * page at most, the nearer to the lengths the better); Lq = the
+ * positions of the step (here never 0 = L: say how many).
+ * Calls that may overlap in time may share a cache that none of them writes (rr_paged_attn without RR_FLAG_ACCUMULATE only
+ * reads); each needs a workspace of its own.  Pages may be shared by sequences (a common beginning) as long as nothing is
+ * written to them: neither rr_paged_write nor RR_FLAG_ACCUMULATE.
+ */
+typedef struct {
+    void* K;
+    void* V;
+    float* weight;
+    const int32_t* table;
+    const int32_t* length;
+    int32_t page, num_pages, width;
+} rr_paged_cache;
+
+/*
+ * The last count[b] of the sequence's length[b] positions are written to their pages: row t < count[b] of K and V
+ * [batch, Hkv, Lq, d] (layout: the q strides of the shape, for both; Hq is not used) goes to position
+ * length[b] - count[b] + t.  So length is set to include the new positions first, and writing twice changes nothing.
+ *   count      [batch] int32 on the device, held to 0 .. Lq; NULL = Lq for every sequence.
+ *   weight     [batch, Hkv, Lq] fp32, contiguous: weights the positions start with (rr_key_weights of a prompt); NULL = 0.
+ *              cache->weight NULL: none are kept (`weight` must be NULL too).
+ * Positions in front of the sequence, or without a page, are not written.  batch * Hkv <= 65535.
+ */
+int rr_paged_write(const rr_shape* shape, const rr_paged_cache* cache, const void* K, const void* V, const int32_t* count,
+                   const float* weight, void* hip_stream);
+
+/*
+ * Attention of the last Lq positions of every sequence (one new token, or a few) against the cache.  Query row t of sequence b
+ * is position length[b] - Lq + t and sees key j iff j <= its position and (window == 0 or j > position - window or
+ * j < sinks); a row that sees none (a sequence of length 0, a position in front of the sequence, pages that are none) gives
+ * O = 0 and lse = -inf.
+ *   window     0 = the whole context, or >= 1 as for rr_window_attn, with sinks >= 0.  (Positions are those of the cache: after
+ *              an eviction they count what is left.)
+ *   flags      0 or RR_FLAG_ACCUMULATE: the weights of every visible position grow by the sum of its softmax weights over the
+ *              Lq rows of the KV head's query heads, cache->weight[page][kv][slot] += sum_rows exp(q k / sqrt(d) - lse).
+ *   lse        optional [batch, Hq, Lq].
+ *   workspace  rr_paged_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards.  (The cache's arrays may be
+ *              NULL there; page, num_pages and width are used.)  0 on an invalid geometry.
+ * The blocks of all sequences are shared out evenly among the workgroups of one launch, whatever the lengths; parts are fp32 and
+ * joined in a fixed order, so equal calls give equal bits.  O is rounded once.
+ */
+#define RR_FLAG_ACCUMULATE 1u
+size_t rr_paged_workspace_bytes(const rr_shape* shape, const rr_paged_cache* cache, int window, int sinks, uint32_t flags);
+int rr_paged_attn(const rr_shape* shape, const void* Q, const rr_paged_cache* cache, int window, int sinks, uint32_t flags,
+                  void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Softmax weights that the keys get from the queries of a call, summed over the queries and over the query heads of a KV head:
+ * weight[b][kv][j] = sum over heads h of the group and rows i with j <= position of i of exp(q_i k_j / sqrt(d) - lse[b][h][i]).
+ *   Q, K       as for rr_dense_attn; with Lq < L the last Lq positions' queries (an observation window at a prompt's end).
+ *   lse        [batch, Hq, Lq] fp32 as rr_dense_attn writes it for the same queries; rows with -inf give nothing.
+ *   weight     [batch, Hkv, L] fp32, contiguous.  Every element is written.
+ * fp32 sums in a fixed order.
+ */
+int rr_key_weights(const rr_shape* shape, const void* Q, const void* K, const float* lse, float* weight, void* hip_stream);
+
+/*
+ * Holds every sequence of a cache to `keep` positions, head by head: of a sequence of n > keep positions each KV head keeps
+ * the first `sinks`, the last `recent`, and of the others the ones with the largest accumulated weight (equal weights: the lower
+ * position; a weight that is NaN counts as the largest, a position without a page as the smallest), keep in all; of n <= keep
+ * all.  Their K, V and weights go, in order, to positions 0, 1, .. of the pages of to_table (pages of the same pools).
+ *   cache      with weight; read.  The source positions are left as they are.
+ *   to_table   [batch, to_width] int32, to_width * page >= min(keep, L).  No page of it may be one that the source tables
+ *              use within their lengths (the rows would overwrite each other in no order); entries outside [0, num_pages) take
+ *              nothing.
+ *   to_length  [batch] int32, receives min(n, keep).  May be the cache's own length array.
+ *   kept       [batch, Hkv, keep] int32, receives the kept source positions in ascending order, -1 behind them.
+ * sinks + recent <= keep (RR_ERR_PARAM).  The q strides, Hq and Lq of the shape are not used (but checked like any other);
+ * batch * Hkv <= 65535.  Values move bit for bit.
+ */
+int rr_cache_evict(const rr_shape* shape, const rr_paged_cache* cache, int keep, int sinks, int recent, const int32_t* to_table,
+                   int to_width, int32_t* to_length, int32_t* kept, void* hip_stream);
 
 /*
  * Caller-made masks: fills mask->row_count and mask->row_list (and mask->row_order when non-NULL) from

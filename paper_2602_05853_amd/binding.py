@@ -24,6 +24,7 @@ RR_QUEUE_WORDS = 160          # int32 words of rr_mask.queue
 RR_BF16, RR_F32 = 0, 1
 RR_FLAG_PROTECT_LAST = 1
 RR_FLAG_DIAGONAL_TOKEN = 2
+RR_FLAG_ACCUMULATE = 1        # flags of rr_paged_attn
 
 RR_OFFSET_HEAD, RR_OFFSET_FIXED, RR_OFFSET_LAYER, RR_OFFSET_HYBRID = 0, 1, 2, 3
 OFFSET_MODES = {"head": RR_OFFSET_HEAD, "fixed": RR_OFFSET_FIXED, "layer": RR_OFFSET_LAYER, "hybrid": RR_OFFSET_HYBRID}
@@ -31,7 +32,8 @@ OFFSET_MODES = {"head": RR_OFFSET_HEAD, "fixed": RR_OFFSET_FIXED, "layer": RR_OF
 EXPORTS = ("rr_version", "rr_status_string", "rr_workspace_bytes", "rr_estimate", "rr_estimate_ex",
            "rr_sparse_attn", "rr_dense_attn", "rr_accuracy_workspace_bytes", "rr_selection_accuracy",
            "rr_mask_from_dense", "rr_dense_attn_packed", "rr_estimate_static", "rr_attn_workspace_bytes",
-           "rr_sparse_attn_ws", "rr_dense_attn_ws")
+           "rr_sparse_attn_ws", "rr_dense_attn_ws", "rr_window_workspace_bytes", "rr_window_attn",
+           "rr_paged_workspace_bytes", "rr_paged_attn", "rr_paged_write", "rr_key_weights", "rr_cache_evict")
 
 
 class rr_shape(C.Structure):
@@ -51,6 +53,11 @@ class rr_estimate_opts(C.Structure):
     _fields_ = [("flags", C.c_uint32), ("offset_mode", C.c_int32), ("layer", C.c_int32),
                 ("sink_blocks", C.c_int32), ("recent_blocks", C.c_int32), ("seq_first", C.c_void_p),
                 ("ksum_capacity", C.c_int32), ("ksum_valid", C.c_int32)]
+
+
+class rr_paged_cache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("weight", C.c_void_p), ("table", C.c_void_p), ("length", C.c_void_p),
+                ("page", C.c_int32), ("num_pages", C.c_int32), ("width", C.c_int32)]
 
 
 def _load() -> C.CDLL:
@@ -96,6 +103,24 @@ def _load() -> C.CDLL:
     lib.rr_dense_attn.restype = C.c_int
     lib.rr_dense_attn.argtypes = [C.POINTER(rr_shape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
                                   C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.rr_window_workspace_bytes.restype = C.c_size_t
+    lib.rr_window_workspace_bytes.argtypes = [C.POINTER(rr_shape), C.c_int, C.c_int]
+    lib.rr_window_attn.restype = C.c_int
+    lib.rr_window_attn.argtypes = [C.POINTER(rr_shape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int,
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.rr_paged_workspace_bytes.restype = C.c_size_t
+    lib.rr_paged_workspace_bytes.argtypes = [C.POINTER(rr_shape), C.POINTER(rr_paged_cache), C.c_int, C.c_int, C.c_uint32]
+    lib.rr_paged_attn.restype = C.c_int
+    lib.rr_paged_attn.argtypes = [C.POINTER(rr_shape), C.c_void_p, C.POINTER(rr_paged_cache), C.c_int, C.c_int, C.c_uint32,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.rr_paged_write.restype = C.c_int
+    lib.rr_paged_write.argtypes = [C.POINTER(rr_shape), C.POINTER(rr_paged_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                   C.c_void_p]
+    lib.rr_key_weights.restype = C.c_int
+    lib.rr_key_weights.argtypes = [C.POINTER(rr_shape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.rr_cache_evict.restype = C.c_int
+    lib.rr_cache_evict.argtypes = [C.POINTER(rr_shape), C.POINTER(rr_paged_cache), C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int,
+                                   C.c_void_p, C.c_void_p, C.c_void_p]
     return lib
 
 
@@ -400,3 +425,217 @@ def rr_mask_from_dense(Q: torch.Tensor, K: torch.Tensor, dense: torch.Tensor, B:
     cm = mask.c_struct()
     _check(lib.rr_mask_from_dense(C.byref(shp), C.byref(cm), _stream_ptr(stream)))
     return mask
+
+
+# ---- window attention, the paged cache, key weights (see the header for what each computes) ----
+
+def _on_device(device: torch.device, *tensors) -> None:
+    """Every tensor of a call lies on the one GPU the call runs on."""
+    if device.type != "cuda":
+        raise RRError(RR_ERR_PARAM)
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise RRError(RR_ERR_PARAM)
+
+
+def _call(device: torch.device, stream: Optional[torch.cuda.Stream], entry, *args) -> None:
+    """entry(*args, stream) with the tensors' device current."""
+    if device.index == torch.cuda.current_device():
+        _check(entry(*args, _stream_ptr(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(entry(*args, _stream_ptr(stream)))
+
+
+def _check_like(t: torch.Tensor, like: torch.Tensor) -> None:
+    if t.shape != like.shape or t.stride() != like.stride() or t.dtype != like.dtype:
+        raise RRError(RR_ERR_SHAPE)
+
+
+def _check_array(t: torch.Tensor, dtype: torch.dtype, shape) -> None:
+    if t.dtype != dtype:
+        raise RRError(RR_ERR_DTYPE)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise RRError(RR_ERR_SHAPE)
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return t.data_ptr() if t is not None else None
+
+
+def _bytes(t: Optional[torch.Tensor]) -> int:
+    return t.numel() * t.element_size() if t is not None else 0
+
+
+def rr_window_workspace_bytes(Q: torch.Tensor, K: torch.Tensor, window: int, sinks: int = 0) -> int:
+    """Bytes of scratch with which rr_window_attn shares a step's keys out among workgroups (0: it does without)."""
+    return lib.rr_window_workspace_bytes(C.byref(make_shape(Q, K)), window, sinks)
+
+
+def rr_window_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, window: int, sinks: int = 0,
+                   O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None, workspace: Optional[torch.Tensor] = None,
+                   seq_first: Optional[torch.Tensor] = None, B: int = 128) -> torch.Tensor:
+    """Causal attention with a sliding window of `window` positions, the first `sinks` ones always visible.  seq_first, B:
+    packed sequences, as for rr_dense_attn_packed."""
+    shp = make_shape(Q, K)
+    if K.dtype != Q.dtype or V.dtype != Q.dtype:
+        raise RRError(RR_ERR_DTYPE)
+    if V.stride() != K.stride() or V.shape != K.shape:
+        raise RRError(RR_ERR_SHAPE)
+    if O is None:
+        O = _output_like(Q)
+    else:
+        _check_like(O, Q)
+    if lse is not None:
+        _check_array(lse, torch.float32, Q.shape[:3])
+    if seq_first is not None:
+        if B < 1:
+            raise RRError(RR_ERR_SHAPE)
+        _check_seq_first(seq_first, _blocks(shp.L, B), Q.device)
+    _on_device(Q.device, K, V, O, lse, workspace)
+    _call(Q.device, stream, lib.rr_window_attn, C.byref(shp), Q.data_ptr(), K.data_ptr(), V.data_ptr(), window, sinks,
+          _ptr(seq_first), B, O.data_ptr(), _ptr(lse), _ptr(workspace), _bytes(workspace))
+    return O
+
+
+@dataclass
+class PagedCache:
+    """A key-value cache in pages (the rr_paged_cache of the C ABI).
+
+    K and V are pools [pages, Hkv, page, d] (any strides with the last dimension contiguous, the same for both); position p of
+    sequence b lies in page table[b, p // page] at slot p % page, and length[b] counts the sequence's positions.  The caller hands
+    out pages and sets table and length; entries outside the pool (-1) are no page."""
+    K: torch.Tensor
+    V: torch.Tensor
+    table: torch.Tensor                    # int32 [batch, width]
+    length: torch.Tensor                   # int32 [batch]
+    weight: Optional[torch.Tensor] = None  # float32 [pages, Hkv, page]: accumulated softmax weights
+
+    @staticmethod
+    def allocate(pages: int, page: int, Hkv: int, d: int, batch: int, width: int, device, dtype=torch.bfloat16,
+                 weight: bool = False) -> "PagedCache":
+        """Uninitialised pools, no pages handed out, every sequence empty."""
+        return PagedCache(torch.empty(pages, Hkv, page, d, dtype=dtype, device=device),
+                          torch.empty(pages, Hkv, page, d, dtype=dtype, device=device),
+                          torch.full((batch, width), -1, dtype=torch.int32, device=device),
+                          torch.zeros(batch, dtype=torch.int32, device=device),
+                          torch.zeros(pages, Hkv, page, dtype=torch.float32, device=device) if weight else None)
+
+    def c_struct(self) -> rr_paged_cache:
+        K, V, table = self.K, self.V, self.table
+        if K.dim() != 4 or table.dim() != 2 or K.stride(3) != 1 or V.stride() != K.stride() or V.shape != K.shape:
+            raise RRError(RR_ERR_SHAPE)
+        if V.dtype != K.dtype:
+            raise RRError(RR_ERR_DTYPE)
+        pages, Hkv, page, _ = K.shape
+        batch, width = table.shape
+        _check_array(table, torch.int32, (batch, width))
+        _check_array(self.length, torch.int32, (batch,))
+        if self.weight is not None:
+            _check_array(self.weight, torch.float32, (pages, Hkv, page))
+        return rr_paged_cache(K.data_ptr(), V.data_ptr(), _ptr(self.weight), table.data_ptr(), self.length.data_ptr(), page, pages,
+                              width)
+
+    def shape(self, rows: torch.Tensor, Hq: int, max_length: Optional[int]) -> rr_shape:
+        """The rr_shape of a call whose query (or new) rows are `rows` [batch, heads, Lq, d]."""
+        K = self.K
+        if rows.dim() != 4 or rows.stride(3) != 1 or rows.shape[0] != self.table.shape[0] or rows.shape[3] != K.shape[3] or \
+                rows.shape[2] < 1:
+            raise RRError(RR_ERR_SHAPE)
+        if rows.dtype != K.dtype:
+            raise RRError(RR_ERR_DTYPE)
+        r, k = rows.stride(), K.stride()
+        L = self.table.shape[1] * K.shape[2] if max_length is None else max_length
+        return rr_shape(rows.shape[0], L, Hq, K.shape[1], K.shape[3], _dtype_code(K), r[0], r[1], r[2], k[0], k[1], k[2],
+                        rows.shape[2])
+
+
+def rr_paged_workspace_bytes(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: int = 0, accumulate: bool = False,
+                             max_length: Optional[int] = None) -> int:
+    shp, c = cache.shape(Q, Q.shape[1], max_length), cache.c_struct()
+    return lib.rr_paged_workspace_bytes(C.byref(shp), C.byref(c), window, sinks, RR_FLAG_ACCUMULATE if accumulate else 0)
+
+
+def rr_paged_attn(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: int = 0, accumulate: bool = False,
+                  max_length: Optional[int] = None, O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention of the last Lq positions of every sequence, Q [batch, Hq, Lq, d], against the cache.  max_length: the most
+    positions a sequence has (default: what the table holds).  Without `workspace` one is allocated."""
+    shp, c = cache.shape(Q, Q.shape[1], max_length), cache.c_struct()
+    flags = RR_FLAG_ACCUMULATE if accumulate else 0
+    if O is None:
+        O = _output_like(Q)
+    else:
+        _check_like(O, Q)
+    if lse is not None:
+        _check_array(lse, torch.float32, Q.shape[:3])
+    _on_device(Q.device, cache.K, cache.V, cache.table, cache.length, cache.weight, O, lse, workspace)
+    if workspace is None:
+        workspace = torch.empty(lib.rr_paged_workspace_bytes(C.byref(shp), C.byref(c), window, sinks, flags), dtype=torch.uint8,
+                                device=Q.device)
+    _call(Q.device, stream, lib.rr_paged_attn, C.byref(shp), Q.data_ptr(), C.byref(c), window, sinks, flags, O.data_ptr(), _ptr(lse),
+          workspace.data_ptr(), _bytes(workspace))
+    return O
+
+
+def rr_paged_write(cache: PagedCache, K: torch.Tensor, V: torch.Tensor, count: Optional[torch.Tensor] = None,
+                   weight: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """The last count[b] (default: all Lq) of the sequences' positions into their pages, from K, V [batch, Hkv, Lq, d]; set
+    cache.length to include them first."""
+    Hkv = cache.K.shape[1]
+    shp, c = cache.shape(K, Hkv, None), cache.c_struct()
+    if K.shape[1] != Hkv or V.shape != K.shape or V.stride() != K.stride():
+        raise RRError(RR_ERR_SHAPE)
+    if V.dtype != K.dtype:
+        raise RRError(RR_ERR_DTYPE)
+    if count is not None:
+        _check_array(count, torch.int32, (K.shape[0],))
+    if weight is not None:
+        _check_array(weight, torch.float32, K.shape[:3])
+    _on_device(K.device, V, count, weight, cache.K, cache.V, cache.table, cache.length, cache.weight)
+    _call(K.device, stream, lib.rr_paged_write, C.byref(shp), C.byref(c), K.data_ptr(), V.data_ptr(), _ptr(count), _ptr(weight))
+
+
+def rr_key_weights(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, out: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """[batch, Hkv, L] fp32: the softmax weights every key gets from the queries Q (the last Lq positions), summed over queries
+    and the heads of a group.  lse [batch, Hq, Lq] as rr_dense_attn writes it for the same queries."""
+    shp = make_shape(Q, K)
+    if K.dtype != Q.dtype:
+        raise RRError(RR_ERR_DTYPE)
+    _check_array(lse, torch.float32, Q.shape[:3])
+    if out is None:
+        out = torch.empty(K.shape[:3], dtype=torch.float32, device=K.device)
+    else:
+        _check_array(out, torch.float32, K.shape[:3])
+    _on_device(Q.device, K, lse, out)
+    _call(Q.device, stream, lib.rr_key_weights, C.byref(shp), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), out.data_ptr())
+    return out
+
+
+def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int = 0, recent: int = 0,
+                   length: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None):
+    """Holds every sequence to `keep` positions by accumulated weight, head by head, into the pages of `table` [batch, width]
+    (of the same pools, none of them in use).  Returns the cache over those pages and the kept source positions [batch, Hkv,
+    keep] (-1 behind the last)."""
+    shp, c = cache.shape(cache.K[:1].expand(cache.table.shape[0], -1, -1, -1), cache.K.shape[1], None), cache.c_struct()
+    batch, Hkv = shp.batch, shp.Hkv
+    if keep < 1:
+        raise RRError(RR_ERR_PARAM)
+    if table.dim() != 2:
+        raise RRError(RR_ERR_SHAPE)
+    _check_array(table, torch.int32, (batch, table.shape[1]))
+    if length is None:
+        length = torch.empty(batch, dtype=torch.int32, device=cache.K.device)
+    else:
+        _check_array(length, torch.int32, (batch,))
+    if kept is None:
+        kept = torch.empty((batch, Hkv, keep), dtype=torch.int32, device=cache.K.device)
+    else:
+        _check_array(kept, torch.int32, (batch, Hkv, keep))
+    _on_device(cache.K.device, cache.V, cache.table, cache.length, cache.weight, table, length, kept)
+    _call(cache.K.device, stream, lib.rr_cache_evict, C.byref(shp), C.byref(c), keep, sinks, recent, table.data_ptr(), table.shape[1],
+          length.data_ptr(), kept.data_ptr())
+    return PagedCache(cache.K, cache.V, table, length, cache.weight), kept

@@ -1,5 +1,6 @@
 // C ABI of the library (see include/rr_attn.h): argument checks on the host, then launches.
 #include "rr_common.hpp"
+#include "rr_check.hpp"
 
 #include <mutex>
 
@@ -39,32 +40,6 @@ namespace {
 
 using namespace rr;
 
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-int check_shape(const rr_shape* s, Geom* g) {
-    if (!s) return RR_ERR_NULL;
-    if (s->dtype != RR_BF16 && s->dtype != RR_F32) return RR_ERR_DTYPE;
-    if (s->batch < 1 || s->L < 1 || s->Hq < 1 || s->Hkv < 1 || s->d < 8) return RR_ERR_SHAPE;
-    if (s->Hq % s->Hkv) return RR_ERR_SHAPE;
-    if (s->d % 8 || s->d > 256) return RR_ERR_SHAPE;
-    const int64_t row = s->dtype == RR_BF16 ? 8 : 4;          // elements per 16 bytes
-    const int64_t st[6] = {s->q_stride_b, s->q_stride_h, s->q_stride_l,
-                           s->kv_stride_b, s->kv_stride_h, s->kv_stride_l};
-    for (int i = 0; i < 6; ++i)
-        if (st[i] < 0 || st[i] % row) return RR_ERR_SHAPE;
-    if (s->q_stride_l < s->d || s->kv_stride_l < s->d) return RR_ERR_SHAPE;
-    g->batch = s->batch; g->L = s->L; g->Hq = s->Hq; g->Hkv = s->Hkv; g->d = s->d;
-    g->G = s->Hq / s->Hkv;
-    if (s->Lq < 0 || s->Lq > s->L) return RR_ERR_SHAPE;
-    g->Lq = s->Lq ? s->Lq : s->L;
-    g->q0 = g->L - g->Lq;
-    g->qoff = 0;
-    g->Lr = g->L;
-    g->qsb = s->q_stride_b; g->qsh = s->q_stride_h; g->qsl = s->q_stride_l;
-    g->ksb = s->kv_stride_b; g->ksh = s->kv_stride_h; g->ksl = s->kv_stride_l;
-    return RR_OK;
-}
-
 // L rounded up, and the start of the query rows rounded down, to whole blocks of B
 int pad_to_blocks(Geom* g, int B) {
     if (B < 1) return RR_ERR_SHAPE;
@@ -83,8 +58,6 @@ int check_blocks(const Geom& g, int S, int B) {
     if (g.L / B > 8192) return RR_ERR_SHAPE;
     return RR_OK;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 bool use_mfma_attn(const Geom& g, int dtype, int B) { return dtype == RR_BF16 && g.d == 128 && B == 128; }
 
@@ -189,7 +162,7 @@ int static_scratch(void** out) {
 
 extern "C" {
 
-RR_API int rr_version(void) { return 500; }
+RR_API int rr_version(void) { return 600; }
 
 RR_API const char* rr_status_string(int status) {
     switch (status) {

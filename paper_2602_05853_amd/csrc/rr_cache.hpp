@@ -1,0 +1,119 @@
+// What the kernels over a key-value cache share: which 128-key blocks a sequence's queries visit, how a launch's workgroups
+// share the blocks of all sequences, and where a position lies.
+#pragma once
+#include "rr_common.hpp"
+
+namespace rr {
+
+namespace {
+
+constexpr int kUnit = 128;                      // keys of a block
+constexpr int kLeastUnits = 2;                  // blocks a workgroup takes at least, where there are as many
+
+#if defined(__HIP_DEVICE_COMPILE__)
+typedef const __attribute__((address_space(4))) int32_t* scalar_words_t;   // read with scalar loads
+#else
+typedef const int32_t* scalar_words_t;                                     // the host pass only parses the kernels
+#endif
+
+// The blocks that a step at the end of `len` positions visits: 0 .. ns - 1, which hold sinks, then those from first_w to the end.
+struct Visit {
+    int len, ns, first_w, n;
+    __host__ __device__ int block(int i) const { return i < ns ? i : first_w + i - ns; }
+};
+__host__ __device__ inline Visit visit_of(int len, int T, int window, int sinks) {
+    Visit v;
+    v.len = len;
+    const long long lo = (long long)len - T - window + 1;           // first key of the earliest query's window
+    v.first_w = lo > 0 ? (int)(lo / kUnit) : 0;
+    const int ns = (int)(((long long)(sinks < len ? sinks : len) + kUnit - 1) / kUnit);
+    v.ns = ns < v.first_w ? ns : v.first_w;
+    v.n = len > 0 ? v.ns + (len - 1) / kUnit - v.first_w + 1 : 0;
+    return v;
+}
+// The most blocks that any length up to L visits.  (Not those of L itself: a window of 128 that ends with a block is one block,
+// one that ends inside a block is two.)
+inline long long most_blocks(int L, int T, int window, int sinks) {
+    const long long all = ((long long)L + kUnit - 1) / kUnit, near = (long long)window + T - 1;
+    const long long some = ((long long)sinks + kUnit - 1) / kUnit + (near + 2 * kUnit - 2) / kUnit;
+    return all < some ? all : some;
+}
+
+__device__ __forceinline__ int length_of(const CacheArgs& c, int b) {
+    if (!c.length) return c.L;
+    const int n = ((scalar_words_t)c.length)[b];
+    return n < 0 ? 0 : (n > c.L ? c.L : n);
+}
+__device__ __forceinline__ Visit visit(const CacheArgs& c, int b) { return visit_of(length_of(c, b), c.T, c.window, c.sinks); }
+
+// The units of a launch, in order: sequence by sequence, `pairs` (KV head and row tile) by pair, block by block.  Workgroup w
+// of W takes units U w / W .. U (w + 1) / W - 1, whatever sequences they belong to, so all end together however uneven the
+// lengths are; the part of a pair that a workgroup computes has slot w + (number of the pair), which is its own: from one
+// part to the next at least one of the two grows.
+// Every workgroup adds the lengths up for itself: thread t the sequences t per .. t per + per - 1, then a scan over threads.
+template <int kThreads> struct Shares {
+    int pre[kThreads + 1];                      // blocks of the sequences in front of thread t's
+    int wave[kThreads / 64];
+    int at;
+};
+template <int kThreads>
+__device__ __forceinline__ int shares_scan(const CacheArgs& c, Shares<kThreads>& s) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int per = (c.batch + kThreads - 1) / kThreads;
+    int own = 0;
+    for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        if (b < c.batch) {
+            int n = c.L;
+            if (c.length) {
+                n = c.length[b];
+                n = n < 0 ? 0 : (n > c.L ? c.L : n);
+            }
+            own += visit_of(n, c.T, c.window, c.sinks).n;
+        }
+    }
+    int sum = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(sum, o);
+        if (lane >= o) sum += up;
+    }
+    if (lane == 63) s.wave[w] = sum;
+    __syncthreads();
+    int front = 0;
+#pragma unroll
+    for (int i = 0; i < kThreads / 64; ++i) front += i < w ? s.wave[i] : 0;
+    s.pre[tid] = front + sum - own;
+    if (tid == kThreads - 1) s.pre[kThreads] = front + sum;
+    __syncthreads();
+    return s.pre[kThreads];
+}
+// The sequence that block `at` (0 <= at < the scan's total) of all sequences belongs to, its first block and its visit.
+template <int kThreads>
+__device__ __forceinline__ int shares_find(const CacheArgs& c, Shares<kThreads>& s, int at, int* base, Visit* v) {
+    const int tid = threadIdx.x;
+    if (s.pre[tid] <= at && at < s.pre[tid + 1]) s.at = tid;
+    __syncthreads();
+    const int per = (c.batch + kThreads - 1) / kThreads;
+    const int chunk = __builtin_amdgcn_readfirstlane(s.at);
+    int b = chunk * per, front = __builtin_amdgcn_readfirstlane(s.pre[chunk]);
+    *v = visit(c, b);
+    while (at >= front + v->n) {
+        front += v->n;
+        *v = visit(c, ++b);
+    }
+    __syncthreads();                            // s.at may be written again
+    *base = front;
+    return b;
+}
+// Workgroups that take part in U units
+__device__ __forceinline__ long long shares_count(long long U, int workgroups) {
+    const long long most = (U + kLeastUnits - 1) / kLeastUnits;
+    return most < workgroups ? most : workgroups;
+}
+// The workgroup of W that has unit u of U
+__device__ __forceinline__ int shares_owner(long long u, long long U, long long W) { return (int)(((u + 1) * W - 1) / U); }
+
+}  // namespace
+
+}  // namespace rr

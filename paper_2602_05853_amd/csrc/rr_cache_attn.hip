@@ -1,0 +1,417 @@
+// Attention of a step (one new token, or a few) over a key-value cache in pages, and over the contiguous keys and values of a
+// step with a sliding window: O_r = sum_j p_rj v_j, p_rj = exp(q_r k_j / sqrt(d)) / sum, over the keys that row r sees.
+//
+// What bounds it: the stream of the visible keys and values, each read once (2 d values per key and KV head against 4 d G T
+// operations on them).  So a workgroup serves all G T rows of a KV head from the same keys (the rows are the columns of
+// matrix tiles, rr_attn_frag.hpp), straight from memory to registers, the next keys requested before the softmax of the
+// present ones; and the blocks of all sequences are dealt out evenly to one round of workgroups (rr_cache.hpp), each of which
+// writes its parts' normalised outputs and log-sum-exps.  A second kernel joins the parts of every row.
+// Arithmetic: fp32 throughout; bf16 scores are exact products summed in fp32, probabilities three exact bf16 terms.
+//
+// A tile of 16 keys lies in one page (pages are multiples of 16 positions), so an address is one page entry, read by a
+// scalar load a step ahead, and the lane's row offsets.  Tiles without a page, or behind the end, are not read.
+//
+// Weights: the first kernel also keeps its scores (4 bytes per row and key against the 4 d and 8 d of a key's K and V), and a
+// third adds exp(score - lse) over the rows of a KV head, in the order of the rows, to the positions' sums.
+#include "rr_cache.hpp"
+#include "rr_attn_frag.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace rr {
+
+namespace {
+
+constexpr int kCacheWorkgroups = 512;                   // two per compute unit, all resident
+
+template <typename T, int NT, int QT, int TL, int KW>
+__global__ void __launch_bounds__(64 * KW, NT > 8 ? 1 : 2)
+k_cache_attn(CacheArgs c) {
+    using F = Frag<T, NT, TL>;
+    constexpr int kThreads = 64 * KW, kQ = 16 * QT, kPitch = 16 * NT + 4;
+    constexpr int kStep = 16 * TL * KW, kSteps = kUnit / kStep;      // keys of the workgroup at once, and trips to a block
+    static_assert(kStep * kSteps == kUnit, "a block is whole steps");
+    __shared__ __align__(16) float s_o[KW][kQ][kPitch];
+    __shared__ float s_ref[KW][kQ], s_l[KW][kQ];
+    __shared__ Shares<kThreads> s_shares;
+    const float NEG_INF = -__builtin_huge_valf();
+
+    const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, gq = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int R = c.G * c.T, pairs = c.Hkv * c.row_tiles;
+
+    const int total = shares_scan(c, s_shares);
+    const long long U = (long long)total * pairs, W = shares_count(U, (int)gridDim.x);
+    if ((long long)blockIdx.x >= W) return;
+    long long u = U * blockIdx.x / W;
+    const long long u_end = U * (blockIdx.x + 1) / W;
+    int base;
+    Visit v;
+    int b = shares_find(c, s_shares, (int)(u / pairs), &base, &v);
+    int pair = (int)((u - (long long)base * pairs) / v.n), i_lo = (int)(u - (long long)base * pairs - (long long)pair * v.n);
+
+    // rows of a tile this lane reads, relative to its first key
+    const long long k_off = (long long)x * c.ksl;
+    long long v_off[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v_off[r] = (long long)(4 * gq + r) * c.ksl;
+
+    while (u < u_end) {
+        const int blocks = (int)min((long long)(v.n - i_lo), u_end - u);
+        const int kv = pair / c.row_tiles, rt = pair - kv * c.row_tiles;
+        const int q_first = v.len - c.T, q_last = v.len - 1;
+
+        // rows that do not exist repeat the last one and are not stored
+        F qf[QT];
+        int qpos[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const int rr = min(kQ * rt + 16 * t + x, R - 1), hl = rr / c.T, tk = rr - hl * c.T;
+            qf[t].load(reinterpret_cast<const T*>(c.Q) + b * c.qsb + (long long)(kv * c.G + hl) * c.qsh + (long long)tk * c.qsl, c.d, gq);
+            qpos[t] = q_first + tk;
+        }
+        const T* K = reinterpret_cast<const T*>(c.K) + (long long)kv * c.ksh;
+        const T* V = reinterpret_cast<const T*>(c.V) + (long long)kv * c.ksh;
+        const int steps = blocks * kSteps;
+        auto first_key = [&](int st, int tl) { return v.block(i_lo + st / kSteps) * kUnit + (st % kSteps) * kStep + 16 * (TL * w + tl); };
+        // page entries of a step, as loaded
+        int entry[TL];
+        auto request = [&](int st) {
+#pragma unroll
+            for (int tl = 0; tl < TL; ++tl) {
+                const int key = first_key(st, tl);
+                entry[tl] = c.table ? ((scalar_words_t)c.table)[(long long)b * c.width + min(key, q_last) / c.page] : 0;
+            }
+        };
+        F kf[TL];
+        int key0[TL], last[TL];                          // first key of a tile; the last of its keys that exists, -1: none does
+        long long at[TL];                                // where the tile begins
+        auto load_keys = [&](int st) {                   // the step's entries are in `entry`
+#pragma unroll
+            for (int tl = 0; tl < TL; ++tl) {
+                key0[tl] = first_key(st, tl);
+                const bool in = key0[tl] < v.len && (!c.table || (unsigned)entry[tl] < (unsigned)c.num_pages);
+                last[tl] = in ? min(15, v.len - 1 - key0[tl]) : -1;
+                at[tl] = c.table ? (long long)entry[tl] * c.psb + (long long)(key0[tl] % c.page) * c.ksl
+                                 : (long long)b * c.psb + (long long)key0[tl] * c.ksl;
+                if (last[tl] == 15) kf[tl].load(K + at[tl] + k_off, c.d, gq);
+                else if (in) kf[tl].load(K + at[tl] + (long long)min(x, last[tl]) * c.ksl, c.d, gq);
+                else kf[tl] = F{};
+            }
+        };
+        f32x4 acc[QT][NT];
+        float ref[QT], lsum[QT];
+        auto walk = [&](auto careful) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                ref[t] = NEG_INF;
+                lsum[t] = 0.f;
+#pragma unroll
+                for (int ch = 0; ch < NT; ++ch) acc[t][ch] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            request(0);
+            load_keys(0);
+            request(min(1, steps - 1));
+            for (int st = 0; st < steps; ++st) {
+                typename F::V vf;
+#pragma unroll
+                for (int tl = 0; tl < TL; ++tl) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (last[tl] == 15) F::load_v(vf, 4 * tl + r, V + at[tl] + v_off[r], c.d, x);
+                        else if (last[tl] >= 0) F::load_v(vf, 4 * tl + r, V + at[tl] + (long long)min(4 * gq + r, last[tl]) * c.ksl, c.d, x);
+                        else F::drop(vf, 4 * tl + r, true);
+                    }
+                }
+                f32x4 s[QT][TL];
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int tl = 0; tl < TL; ++tl) s[t][tl] = f32x4{0.f, 0.f, 0.f, 0.f};
+                F::template qk<QT>(s, kf, qf);
+                int key_now[TL], last_now[TL];
+#pragma unroll
+                for (int tl = 0; tl < TL; ++tl) {
+                    key_now[tl] = key0[tl];
+                    last_now[tl] = last[tl];
+                    const bool whole = last[tl] == 15 && key0[tl] + 15 <= q_first &&
+                                       (key0[tl] > q_last - c.window || key0[tl] + 15 < c.sinks);
+                    if (!whole) {
+#pragma unroll
+                        for (int t = 0; t < QT; ++t)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int k = 4 * gq + r, key = key0[tl] + k;
+                                const bool sees = k <= last[tl] && key <= qpos[t] && (key > qpos[t] - c.window || key < c.sinks);
+                                s[t][tl][r] = sees ? s[t][tl][r] : NEG_INF;
+                            }
+                    }
+                    if (c.scores) {
+                        const int rows = min(R, kQ);
+                        float* out = c.scores + (u + st / kSteps) * (long long)rows * kUnit + (st % kSteps) * kStep + 16 * (TL * w + tl) + 4 * gq;
+#pragma unroll
+                        for (int t = 0; t < QT; ++t)
+                            if (16 * t + x < rows) *reinterpret_cast<f32x4*>(out + (16 * t + x) * kUnit) = s[t][tl];
+                    }
+                }
+                // the next step's keys travel during the softmax and the second product, the entries behind them through
+                // the next step (the careful walk has no registers for it)
+                auto ahead = [&]() {
+                    if (st + 1 < steps) {
+                        load_keys(st + 1);
+                        request(min(st + 2, steps - 1));
+                    }
+                };
+                if (!decltype(careful)::value) ahead();
+                float p[QT][4 * TL];
+#pragma unroll
+                for (int t = 0; t < QT; ++t) frag_softmax<TL, NT>(s[t], c.scale_log2, ref[t], lsum[t], acc[t], p[t]);
+                if constexpr (decltype(careful)::value) {
+                    // values of keys that no row sees are left out
+#pragma unroll
+                    for (int tl = 0; tl < TL; ++tl)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int k = 4 * gq + r, key = key_now[tl] + k;
+                            F::drop(vf, 4 * tl + r, k > last_now[tl] || key > q_last || !(key > q_first - c.window || key < c.sinks));
+                        }
+                }
+                F::template pv<QT, decltype(careful)::value>(acc, vf, p);
+                if (decltype(careful)::value) ahead();
+            }
+        };
+        walk(std::false_type{});
+        if (has_nan(acc)) walk(std::true_type{});
+
+        // the waves' shares, brought to one reference: the part's normalised output and log2 of its sum of exponentials
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            float l = lsum[t];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (gq == 0) { s_ref[w][16 * t + x] = ref[t]; s_l[w][16 * t + x] = l; }
+            frag_store<F::kW, NT>(acc[t], &s_o[w][16 * t + x][0], gq);
+        }
+        __syncthreads();
+        const long long slot = blockIdx.x + (long long)b * pairs + pair;
+        for (int idx = tid; idx < kQ * 4 * NT; idx += kThreads) {
+            const int q = idx / (4 * NT), ch = 4 * (idx - q * (4 * NT));
+            if (kQ * rt + q >= R || ch >= c.d) continue;
+            float top = NEG_INF;
+#pragma unroll
+            for (int i = 0; i < KW; ++i) top = fmaxf(top, s_ref[i][q]);
+            float l = 0.f;
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KW; ++i) {
+                const float f = s_ref[i][q] == NEG_INF ? 0.f : __builtin_amdgcn_exp2f(s_ref[i][q] - top);
+                l = fmaf(f, s_l[i][q], l);
+                const f32x4 part = *reinterpret_cast<const f32x4*>(&s_o[i][q][ch]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, part[e], o[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = l > 0.f ? o[e] / l : 0.f;
+            *reinterpret_cast<f32x4*>(c.part_O + (slot * kQ + q) * c.d + ch) = o;
+            if (ch == 0) c.part_lse[slot * kQ + q] = l > 0.f ? top + log2f(l) : NEG_INF;
+        }
+        __syncthreads();                                 // the shares' places are free again
+
+        u += blocks;
+        i_lo += blocks;
+        if (i_lo == v.n && u < u_end) {
+            i_lo = 0;
+            if (++pair == pairs) {
+                pair = 0;
+                do v = visit(c, ++b); while (v.n == 0);  // (units are left, so a sequence that has some follows)
+            }
+        }
+    }
+}
+
+// One workgroup per query row: O = sum_p w_p O_p / sum_p w_p with w_p = 2^(lse_p - max), rounded once.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_cache_join(CacheArgs c, int row_tile, int workgroups) {
+    __shared__ Shares<256> s_shares;
+    __shared__ float s_w[kCacheWorkgroups];
+    __shared__ float s_red[4];
+    __shared__ float s_o[4][256];
+    const float NEG_INF = -__builtin_huge_valf();
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int R = c.G * c.T, pairs = c.Hkv * c.row_tiles;
+    int row = blockIdx.x;                                // (b, kv, r)
+    const int r = row % R, kv = row / R % c.Hkv, b = row / R / c.Hkv;
+    const int pair = kv * c.row_tiles + r / row_tile;
+
+    const int total = shares_scan(c, s_shares);
+    const long long U = (long long)total * pairs, W = shares_count(U, workgroups);
+    const Visit v = visit(c, b);
+    int parts = 0;
+    long long first = 0;
+    if (v.n > 0) {
+        // blocks in front of sequence b
+        const int per = (c.batch + 255) / 256;
+        int front = s_shares.pre[b / per];
+        for (int i = b / per * per; i < b; ++i) front += visit(c, i).n;
+        const long long u = (long long)front * pairs + (long long)pair * v.n;
+        first = shares_owner(u, U, W);
+        parts = (int)(shares_owner(u + v.n - 1, U, W) - first) + 1;
+    }
+    const long long slot = first + (long long)b * pairs + pair;
+    const float* lse = c.part_lse + slot * row_tile + r % row_tile;
+    const float* O = c.part_O + (slot * row_tile + r % row_tile) * c.d;
+
+    float mx = NEG_INF;
+    for (int p = tid; p < parts; p += 256) {
+        const float l = lse[(long long)p * row_tile];
+        s_w[p] = l;
+        mx = fmaxf(mx, l);
+    }
+    mx = wave_max(mx);
+    if (lane == 0) s_red[wv] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+    for (int p = tid; p < parts; p += 256) s_w[p] = s_w[p] == NEG_INF ? 0.f : __builtin_amdgcn_exp2f(s_w[p] - mx);
+    __syncthreads();
+
+    // wave wv takes the parts wv, wv + 4, ..; a lane the channels lane, lane + 64, ..
+    float den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int p = wv; p < parts; p += 4) {
+        const float wp = s_w[p];
+        if (wp == 0.f) continue;                         // (whatever it holds)
+        den += wp;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (64 * k + lane < c.d) o[k] = fmaf(wp, O[(long long)p * row_tile * c.d + 64 * k + lane], o[k]);
+    }
+    if (lane == 0) s_red[wv] = den;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s_o[wv][64 * k + lane] = o[k];
+    __syncthreads();
+    den = s_red[0] + s_red[1] + s_red[2] + s_red[3];
+    const float inv = den > 0.f ? 1.0f / den : 0.f;
+    const int hl = r / c.T, tk = r - hl * c.T, h = kv * c.G + hl;
+    if (tid < c.d) {
+        const float sum = (s_o[0][tid] + s_o[1][tid]) + (s_o[2][tid] + s_o[3][tid]);
+        T* out = reinterpret_cast<T*>(c.O) + b * c.qsb + h * c.qsh + tk * c.qsl;
+        Elem<T>::store1(out + tid, sum * inv);
+    }
+    if (tid == 0) {
+        const float l2 = mx + log2f(den);
+        if (c.lse) c.lse[((long long)b * c.Hq + h) * c.T + tk] = den > 0.f ? l2 * 0.6931471805599453f : NEG_INF;
+        if (c.row_lse) c.row_lse[row] = den > 0.f ? l2 : -NEG_INF;
+    }
+}
+
+// weight[page][kv][slot] += sum over the KV head's rows of 2^(score - lse), a thread to a position.
+__global__ void __launch_bounds__(256)
+k_cache_weights(CacheArgs c, int row_tile) {
+    __shared__ Shares<256> s_shares;
+    const int R = c.G * c.T, rows = min(R, row_tile);
+    const int total = shares_scan(c, s_shares);
+    // two blocks of (sequence, KV head) to a trip; trips are dealt out evenly
+    const long long items = (long long)total * c.Hkv;
+    long long i = items * blockIdx.x / gridDim.x;
+    const long long end = items * (blockIdx.x + 1) / gridDim.x;
+    if (i >= end) return;
+    int base;
+    Visit v;
+    int b = shares_find(c, s_shares, (int)(i / c.Hkv), &base, &v);
+    int kv = (int)((i - (long long)base * c.Hkv) / v.n), blk = (int)(i - (long long)base * c.Hkv - (long long)kv * v.n);
+    const int half = threadIdx.x >> 7, k = threadIdx.x & 127;
+    while (i < end) {
+        const int n = (int)min((long long)(v.n - blk), end - i);
+        for (int j = half; j < n; j += 2) {
+            const int pos = v.block(blk + j) * kUnit + k;
+            if (pos >= v.len) continue;
+            const int e = c.table[(long long)b * c.width + pos / c.page];
+            if ((unsigned)e >= (unsigned)c.num_pages) continue;
+            float sum = 0.f;
+            for (int rt = 0; rt < c.row_tiles; ++rt) {
+                const long long u = (long long)base * c.Hkv * c.row_tiles + (long long)(kv * c.row_tiles + rt) * v.n + blk + j;
+                const float* s = c.scores + u * rows * kUnit + k;
+                const float* l = c.row_lse + ((long long)b * c.Hkv + kv) * R + rt * row_tile;
+                const int here = min(rows, R - rt * row_tile);
+                for (int q = 0; q < here; ++q) sum += __builtin_amdgcn_exp2f(fmaf(s[q * kUnit], c.scale_log2, -l[q]));
+            }
+            float* out = c.weight + ((long long)e * c.Hkv + kv) * c.page + pos % c.page;
+            *out += sum;
+        }
+        i += n;
+        blk += n;
+        if (blk == v.n && i < end) {
+            blk = 0;
+            if (++kv == c.Hkv) {
+                kv = 0;
+                do {
+                    base += v.n;
+                    v = visit(c, ++b);
+                } while (v.n == 0);
+            }
+        }
+    }
+}
+
+int row_tile_of(const CacheArgs& c, int dtype) { return dtype == RR_BF16 && c.d == 128 && c.G * c.T > 16 ? 32 : 16; }
+
+}  // namespace
+
+bool cache_attn_plan(const CacheArgs& c, int dtype, bool accumulate, CachePlan* p) {
+    const long long R = (long long)c.G * c.T;
+    if (R > (1 << 24)) return false;
+    p->row_tile = row_tile_of(c, dtype);
+    p->row_tiles = (int)((R + p->row_tile - 1) / p->row_tile);
+    const long long pairs = (long long)c.Hkv * p->row_tiles, blocks = most_blocks(c.L, c.T, c.window, c.sinks);
+    // the sums of blocks and the indexes of pairs and rows are 32 bits
+    if ((long long)c.batch * blocks > 0x7fffffff || c.batch * pairs > 0x7fffffff || c.batch * c.Hkv * R > 0x7fffffff) return false;
+    const long long U = c.batch * blocks * pairs;
+    const long long W = std::min<long long>(kCacheWorkgroups, (U + kLeastUnits - 1) / kLeastUnits);
+    p->workgroups = (int)std::max(1ll, W);
+    const long long slots = p->workgroups + c.batch * pairs;
+    p->part_rows = (size_t)slots * p->row_tile;
+    p->part_bytes = (p->part_rows * (c.d + 1) * sizeof(float) + 255) / 256 * 256;
+    p->score_bytes = accumulate ? (size_t)U * (size_t)std::min<long long>(R, p->row_tile) * kUnit * sizeof(float) : 0;
+    p->row_bytes = accumulate ? ((size_t)c.batch * c.Hkv * R * sizeof(float) + 255) / 256 * 256 : 0;
+    return true;
+}
+
+hipError_t launch_cache_attn(const CacheArgs& c, int dtype, const CachePlan& plan, hipStream_t st) {
+    auto launch = [&](auto kernel, int waves) -> hipError_t {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(64 * waves), 0, st, c);
+        return hipGetLastError();
+    };
+    auto pick = [&](auto tiles) -> hipError_t {
+        constexpr int N = decltype(tiles)::value;
+        if (dtype == RR_BF16) {
+            if constexpr (N == 8)
+                if (plan.row_tile == 32) return launch(k_cache_attn<bf16_t, N, 2, 2, 4>, 4);
+            return launch(k_cache_attn<bf16_t, N, 1, 2, 4>, 4);
+        }
+        if constexpr (N > 8) return launch(k_cache_attn<float, N, 1, 1, 4>, 4);
+        else return launch(k_cache_attn<float, N, 1, 1, 8>, 8);
+    };
+    using std::integral_constant;
+    hipError_t e = hipErrorInvalidValue;
+    switch ((c.d + 15) / 16) {
+#define RR_CACHE_CASE(N) case N: e = pick(integral_constant<int, N>{}); break
+        RR_CACHE_CASE(1); RR_CACHE_CASE(2); RR_CACHE_CASE(3); RR_CACHE_CASE(4);
+        RR_CACHE_CASE(5); RR_CACHE_CASE(6); RR_CACHE_CASE(7); RR_CACHE_CASE(8);
+        RR_CACHE_CASE(9); RR_CACHE_CASE(10); RR_CACHE_CASE(11); RR_CACHE_CASE(12);
+        RR_CACHE_CASE(13); RR_CACHE_CASE(14); RR_CACHE_CASE(15); RR_CACHE_CASE(16);
+#undef RR_CACHE_CASE
+        default: break;
+    }
+    if (e != hipSuccess) return e;
+    const dim3 rows((unsigned)(c.batch * c.Hkv * c.G * c.T));
+    if (dtype == RR_BF16) hipLaunchKernelGGL(k_cache_join<bf16_t>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
+    else hipLaunchKernelGGL(k_cache_join<float>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
+    e = hipGetLastError();
+    if (e != hipSuccess || !c.scores) return e;
+    const long long items = c.batch * most_blocks(c.L, c.T, c.window, c.sinks) * c.Hkv;
+    hipLaunchKernelGGL(k_cache_weights, dim3((unsigned)std::min(1024ll, (items + 1) / 2)), dim3(256), 0, st, c, plan.row_tile);
+    return hipGetLastError();
+}
+
+}  // namespace rr

@@ -194,6 +194,66 @@ constexpr int kMaxOrderedRows = 32768;   // G * Nb up to which a row order is pr
 hipError_t launch_attn_generic(const Geom& g, int dtype, const AttnArgs& a, hipStream_t st);
 hipError_t launch_attn_mfma_bf16(const Geom& g, const AttnArgs& a, hipStream_t st);
 
+// (5) causal attention with a sliding window: key j reaches the query at position i where j <= i and (j > i - window or
+// j - s0 < sinks), s0 the first position of the query's sequence (packed sequences: blocks of B; otherwise 0).
+struct WindowArgs {
+    const void* Q; const void* K; const void* V; void* O; float* lse;
+    int window, sinks;
+    const int32_t* seq_first;   // packed sequences, as in AttnArgs; nullptr = one sequence
+    int B;
+};
+hipError_t launch_window_generic(const Geom& g, int dtype, const WindowArgs& a, hipStream_t st);
+
+// (6) a key-value cache in pages, or the contiguous keys and values of a step (table and length nullptr, page 0).
+struct CacheArgs {
+    int batch, Hq, Hkv, G, d;
+    int T;                      // query positions: the last T of every sequence
+    int L;                      // lengths are held to 0 .. L
+    long long qsb, qsh, qsl;    // Q and O
+    long long psb;              // elements from page to page (contiguous: from batch entry to batch entry)
+    long long ksh, ksl;
+    const void* Q; const void* K; const void* V; void* O; float* lse;
+    float* weight;              // [num_pages][Hkv][page]
+    const int32_t* table;       // [batch][width]
+    const int32_t* length;      // [batch]
+    int page, num_pages, width;
+    int window, sinks;          // as above; window = L + T: the whole context
+    float scale_log2;           // log2(e) / sqrt(d)
+    // of a launch
+    int row_tiles;              // a KV head's G T rows, so many at a time
+    float* part_O; float* part_lse;   // [slot][rows of a tile][d] and [slot][rows of a tile], fp32, log2 units
+    float* scores;              // [unit][rows of a tile][128]: products with the keys of 128 positions, -inf where masked; or nullptr
+    float* row_lse;             // [batch][Hkv][G T], log2 units, +inf for a row without a key: read by the sums of the weights
+};
+struct CachePlan {
+    int row_tile, row_tiles;    // rows to a workgroup, and how many such tiles a KV head has
+    int workgroups;
+    size_t part_rows;           // rows of partial results
+    size_t part_bytes, score_bytes, row_bytes;
+    size_t total() const { return part_bytes + score_bytes + row_bytes; }
+};
+// what a call takes of its workspace; false: more than the indexes of a launch hold
+bool cache_attn_plan(const CacheArgs& c, int dtype, bool accumulate, CachePlan* plan);
+hipError_t launch_cache_attn(const CacheArgs& c, int dtype, const CachePlan& plan, hipStream_t st);
+
+// (7) new positions into their pages; (8) a cache's positions by weight into other pages.
+struct CacheWriteArgs {
+    const void* K; const void* V; const float* weight;   // [batch][Hkv][T][d] by qs*; [batch][Hkv][T] or nullptr
+    const int32_t* count;                                // [batch], or nullptr: all T
+};
+hipError_t launch_cache_write(const CacheArgs& c, int dtype, const CacheWriteArgs& a, void* K, void* V, hipStream_t st);
+struct CacheEvictArgs {
+    int keep, sinks, recent;
+    const int32_t* to;          // [batch][to_width]
+    int to_width;
+    int32_t* to_length;
+    int32_t* kept;              // [batch][Hkv][keep]
+};
+hipError_t launch_cache_evict(const CacheArgs& c, int dtype, const CacheEvictArgs& a, void* K, void* V, hipStream_t st);
+
+// (9) softmax weights that every key gets from the queries of a call: out[b][kv][key], fp32.
+hipError_t launch_key_weights(const Geom& g, int dtype, const void* Q, const void* K, const float* lse, float* out, hipStream_t st);
+
 // Raises a kernel's dynamic-LDS limit on the current device to at least `bytes`.  The limit is per (kernel,
 // device) and only ever grows, so the runtime is asked once per pair and size, not on every launch.
 hipError_t allow_dynamic_lds(const void* kernel, size_t bytes);
