@@ -406,9 +406,13 @@ int rr_paged_attn(const rr_shape* shape, const void* Q, const rr_paged_cache* ca
  *   Q, K       as for rr_dense_attn; with Lq < L the last Lq positions' queries (an observation window at a prompt's end).
  *   lse        [batch, Hq, Lq] fp32 as rr_dense_attn writes it for the same queries; rows with -inf give nothing.
  *   weight     [batch, Hkv, L] fp32, contiguous.  Every element is written.
+ *   workspace  rr_key_weights_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards; NULL where that is 0
+ *              (many keys, or few queries).
  * fp32 sums in a fixed order.
  */
-int rr_key_weights(const rr_shape* shape, const void* Q, const void* K, const float* lse, float* weight, void* hip_stream);
+size_t rr_key_weights_workspace_bytes(const rr_shape* shape);
+int rr_key_weights(const rr_shape* shape, const void* Q, const void* K, const float* lse, float* weight, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
 
 /*
  * Holds every sequence of a cache to `keep` positions, head by head: of a sequence of n > keep positions each KV head keeps

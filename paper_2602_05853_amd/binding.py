@@ -33,7 +33,8 @@ EXPORTS = ("rr_version", "rr_status_string", "rr_workspace_bytes", "rr_estimate"
            "rr_sparse_attn", "rr_dense_attn", "rr_accuracy_workspace_bytes", "rr_selection_accuracy",
            "rr_mask_from_dense", "rr_dense_attn_packed", "rr_estimate_static", "rr_attn_workspace_bytes",
            "rr_sparse_attn_ws", "rr_dense_attn_ws", "rr_window_workspace_bytes", "rr_window_attn",
-           "rr_paged_workspace_bytes", "rr_paged_attn", "rr_paged_write", "rr_key_weights", "rr_cache_evict")
+           "rr_paged_workspace_bytes", "rr_paged_attn", "rr_paged_write", "rr_key_weights", "rr_cache_evict",
+           "rr_key_weights_workspace_bytes")
 
 
 class rr_shape(C.Structure):
@@ -117,7 +118,10 @@ def _load() -> C.CDLL:
     lib.rr_paged_write.argtypes = [C.POINTER(rr_shape), C.POINTER(rr_paged_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                    C.c_void_p]
     lib.rr_key_weights.restype = C.c_int
-    lib.rr_key_weights.argtypes = [C.POINTER(rr_shape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.rr_key_weights.argtypes = [C.POINTER(rr_shape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                   C.c_void_p]
+    lib.rr_key_weights_workspace_bytes.restype = C.c_size_t
+    lib.rr_key_weights_workspace_bytes.argtypes = [C.POINTER(rr_shape)]
     lib.rr_cache_evict.restype = C.c_int
     lib.rr_cache_evict.argtypes = [C.POINTER(rr_shape), C.POINTER(rr_paged_cache), C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int,
                                    C.c_void_p, C.c_void_p, C.c_void_p]
@@ -597,10 +601,15 @@ def rr_paged_write(cache: PagedCache, K: torch.Tensor, V: torch.Tensor, count: O
     _call(K.device, stream, lib.rr_paged_write, C.byref(shp), C.byref(c), K.data_ptr(), V.data_ptr(), _ptr(count), _ptr(weight))
 
 
+def rr_key_weights_workspace_bytes(Q: torch.Tensor, K: torch.Tensor) -> int:
+    return lib.rr_key_weights_workspace_bytes(C.byref(make_shape(Q, K)))
+
+
 def rr_key_weights(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, out: Optional[torch.Tensor] = None,
-                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """[batch, Hkv, L] fp32: the softmax weights every key gets from the queries Q (the last Lq positions), summed over queries
-    and the heads of a group.  lse [batch, Hq, Lq] as rr_dense_attn writes it for the same queries."""
+    and the heads of a group.  lse [batch, Hq, Lq] as rr_dense_attn writes it for the same queries.  Without `workspace` one is
+    allocated where it is needed."""
     shp = make_shape(Q, K)
     if K.dtype != Q.dtype:
         raise RRError(RR_ERR_DTYPE)
@@ -609,8 +618,12 @@ def rr_key_weights(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, out: Opt
         out = torch.empty(K.shape[:3], dtype=torch.float32, device=K.device)
     else:
         _check_array(out, torch.float32, K.shape[:3])
-    _on_device(Q.device, K, lse, out)
-    _call(Q.device, stream, lib.rr_key_weights, C.byref(shp), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), out.data_ptr())
+    _on_device(Q.device, K, lse, out, workspace)
+    if workspace is None:
+        n = lib.rr_key_weights_workspace_bytes(C.byref(shp))
+        workspace = torch.empty(n, dtype=torch.uint8, device=Q.device) if n else None
+    _call(Q.device, stream, lib.rr_key_weights, C.byref(shp), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), out.data_ptr(),
+          _ptr(workspace), _bytes(workspace))
     return out
 
 

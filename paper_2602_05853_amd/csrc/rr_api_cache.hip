@@ -24,6 +24,16 @@ int check_window(const rr_shape* shape, int window, int sinks, Geom* g) {
     return RR_OK;
 }
 
+int check_key_weights(const rr_shape* shape, Geom* g) {
+    const int rc = check_shape(shape, g);
+    if (rc != RR_OK) return rc;
+    // the indexes of a launch (tiles of 128 keys and more), and of a KV head's stages of 32 rows, are 32 bits
+    if (g->L > kMostPositions || (long long)g->batch * g->Hkv > 0x7fffffff || (long long)g->G * ((g->Lq + 31) / 32) > 0x3fffffff ||
+        (long long)g->batch * g->Hkv * ((g->L + 127) / 128) > 0x7fffff)
+        return RR_ERR_SHAPE;
+    return RR_OK;
+}
+
 // A step of few rows per KV head whose keys are shared out among workgroups, contiguous form of the cache kernels
 bool window_step(const Geom& g, int dtype, int window, int sinks, CacheArgs* c, CachePlan* plan) {
     if (g.Lq > 16 || g.G * g.Lq > 32) return false;
@@ -173,19 +183,26 @@ RR_API int rr_cache_evict(const rr_shape* shape, const rr_paged_cache* cache, in
     if (keep < 1 || sinks < 0 || recent < 0 || (long long)sinks + recent > keep) return RR_ERR_PARAM;
     // a target holds what is kept of the longest sequence
     if (to_width < 1 || (long long)to_width * c.page < std::min(keep, c.L)) return RR_ERR_SHAPE;
-    if ((long long)c.batch * c.Hkv > 65535) return RR_ERR_SHAPE;
+    if (!aligned16(cache->weight) || (long long)c.batch * c.Hkv > 65535) return RR_ERR_SHAPE;
     const CacheEvictArgs a = {keep, sinks, recent, to_table, to_width, to_length, kept};
     return launch_cache_evict(c, shape->dtype, a, cache->K, cache->V, (hipStream_t)hip_stream) == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
 }
 
-RR_API int rr_key_weights(const rr_shape* shape, const void* Q, const void* K, const float* lse, float* weight, void* hip_stream) {
+RR_API size_t rr_key_weights_workspace_bytes(const rr_shape* shape) {
     Geom g;
-    const int rc = check_shape(shape, &g);
+    return check_key_weights(shape, &g) == RR_OK ? key_weights_bytes(g, shape->dtype) : 0;
+}
+
+RR_API int rr_key_weights(const rr_shape* shape, const void* Q, const void* K, const float* lse, float* weight, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+    Geom g;
+    const int rc = check_key_weights(shape, &g);
     if (rc != RR_OK) return rc;
     if (!Q || !K || !lse || !weight) return RR_ERR_NULL;
-    if (g.L > kMostPositions || g.batch > 65535 || g.Hkv > 65535) return RR_ERR_SHAPE;
     if (!aligned16(Q) || !aligned16(K)) return RR_ERR_SHAPE;
-    return launch_key_weights(g, shape->dtype, Q, K, lse, weight, (hipStream_t)hip_stream) == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
+    const size_t need = key_weights_bytes(g, shape->dtype);
+    if (need && (!workspace || workspace_bytes < need || misaligned256(workspace))) return RR_ERR_WORKSPACE;
+    return launch_key_weights(g, shape->dtype, Q, K, lse, weight, workspace, (hipStream_t)hip_stream) == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
 }
 
 }  // extern "C"

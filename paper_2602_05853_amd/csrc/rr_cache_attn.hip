@@ -25,7 +25,9 @@ namespace {
 
 constexpr int kCacheWorkgroups = 512;                   // two per compute unit, all resident
 
-template <typename T, int NT, int QT, int TL, int KW>
+// D: d where it fills the matrix tiles, so that a row's last channels need no check (which would wait for the keys in front of
+// the work they are requested ahead of), or 0.
+template <typename T, int NT, int D, int QT, int TL, int KW>
 __global__ void __launch_bounds__(64 * KW, NT > 8 ? 1 : 2)
 k_cache_attn(CacheArgs c) {
     using F = Frag<T, NT, TL>;
@@ -36,6 +38,7 @@ k_cache_attn(CacheArgs c) {
     __shared__ float s_ref[KW][kQ], s_l[KW][kQ];
     __shared__ Shares<kThreads> s_shares;
     const float NEG_INF = -__builtin_huge_valf();
+    const int d = D ? D : c.d;
 
     const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, gq = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -68,7 +71,7 @@ k_cache_attn(CacheArgs c) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const int rr = min(kQ * rt + 16 * t + x, R - 1), hl = rr / c.T, tk = rr - hl * c.T;
-            qf[t].load(reinterpret_cast<const T*>(c.Q) + b * c.qsb + (long long)(kv * c.G + hl) * c.qsh + (long long)tk * c.qsl, c.d, gq);
+            qf[t].load(reinterpret_cast<const T*>(c.Q) + b * c.qsb + (long long)(kv * c.G + hl) * c.qsh + (long long)tk * c.qsl, d, gq);
             qpos[t] = q_first + tk;
         }
         const T* K = reinterpret_cast<const T*>(c.K) + (long long)kv * c.ksh;
@@ -95,8 +98,8 @@ k_cache_attn(CacheArgs c) {
                 last[tl] = in ? min(15, v.len - 1 - key0[tl]) : -1;
                 at[tl] = c.table ? (long long)entry[tl] * c.psb + (long long)(key0[tl] % c.page) * c.ksl
                                  : (long long)b * c.psb + (long long)key0[tl] * c.ksl;
-                if (last[tl] == 15) kf[tl].load(K + at[tl] + k_off, c.d, gq);
-                else if (in) kf[tl].load(K + at[tl] + (long long)min(x, last[tl]) * c.ksl, c.d, gq);
+                if (last[tl] == 15) kf[tl].load(K + at[tl] + k_off, d, gq);
+                else if (in) kf[tl].load(K + at[tl] + (long long)min(x, last[tl]) * c.ksl, d, gq);
                 else kf[tl] = F{};
             }
         };
@@ -119,8 +122,8 @@ k_cache_attn(CacheArgs c) {
                 for (int tl = 0; tl < TL; ++tl) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        if (last[tl] == 15) F::load_v(vf, 4 * tl + r, V + at[tl] + v_off[r], c.d, x);
-                        else if (last[tl] >= 0) F::load_v(vf, 4 * tl + r, V + at[tl] + (long long)min(4 * gq + r, last[tl]) * c.ksl, c.d, x);
+                        if (last[tl] == 15) F::load_v(vf, 4 * tl + r, V + at[tl] + v_off[r], d, x);
+                        else if (last[tl] >= 0) F::load_v(vf, 4 * tl + r, V + at[tl] + (long long)min(4 * gq + r, last[tl]) * c.ksl, d, x);
                         else F::drop(vf, 4 * tl + r, true);
                     }
                 }
@@ -197,7 +200,7 @@ k_cache_attn(CacheArgs c) {
         const long long slot = blockIdx.x + (long long)b * pairs + pair;
         for (int idx = tid; idx < kQ * 4 * NT; idx += kThreads) {
             const int q = idx / (4 * NT), ch = 4 * (idx - q * (4 * NT));
-            if (kQ * rt + q >= R || ch >= c.d) continue;
+            if (kQ * rt + q >= R || ch >= d) continue;
             float top = NEG_INF;
 #pragma unroll
             for (int i = 0; i < KW; ++i) top = fmaxf(top, s_ref[i][q]);
@@ -213,7 +216,7 @@ k_cache_attn(CacheArgs c) {
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = l > 0.f ? o[e] / l : 0.f;
-            *reinterpret_cast<f32x4*>(c.part_O + (slot * kQ + q) * c.d + ch) = o;
+            *reinterpret_cast<f32x4*>(c.part_O + (slot * kQ + q) * d + ch) = o;
             if (ch == 0) c.part_lse[slot * kQ + q] = l > 0.f ? top + log2f(l) : NEG_INF;
         }
         __syncthreads();                                 // the shares' places are free again
@@ -382,20 +385,21 @@ hipError_t launch_cache_attn(const CacheArgs& c, int dtype, const CachePlan& pla
         hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(64 * waves), 0, st, c);
         return hipGetLastError();
     };
-    auto pick = [&](auto tiles) -> hipError_t {
-        constexpr int N = decltype(tiles)::value;
+    auto pick = [&](auto tiles, auto full) -> hipError_t {
+        constexpr int N = decltype(tiles)::value, D = decltype(full)::value;
         if (dtype == RR_BF16) {
-            if constexpr (N == 8)
-                if (plan.row_tile == 32) return launch(k_cache_attn<bf16_t, N, 2, 2, 4>, 4);
-            return launch(k_cache_attn<bf16_t, N, 1, 2, 4>, 4);
+            if constexpr (D == 128)
+                if (plan.row_tile == 32) return launch(k_cache_attn<bf16_t, N, D, 2, 2, 4>, 4);
+            return launch(k_cache_attn<bf16_t, N, D, 1, 2, 4>, 4);
         }
-        if constexpr (N > 8) return launch(k_cache_attn<float, N, 1, 1, 4>, 4);
-        else return launch(k_cache_attn<float, N, 1, 1, 8>, 8);
+        if constexpr (N > 8) return launch(k_cache_attn<float, N, D, 1, 1, 4>, 4);
+        else return launch(k_cache_attn<float, N, D, 1, 1, 8>, 8);
     };
     using std::integral_constant;
     hipError_t e = hipErrorInvalidValue;
     switch ((c.d + 15) / 16) {
-#define RR_CACHE_CASE(N) case N: e = pick(integral_constant<int, N>{}); break
+#define RR_CACHE_CASE(N) case N: e = c.d == 16 * N ? pick(integral_constant<int, N>{}, integral_constant<int, 16 * N>{}) \
+                                             : pick(integral_constant<int, N>{}, integral_constant<int, 0>{}); break
         RR_CACHE_CASE(1); RR_CACHE_CASE(2); RR_CACHE_CASE(3); RR_CACHE_CASE(4);
         RR_CACHE_CASE(5); RR_CACHE_CASE(6); RR_CACHE_CASE(7); RR_CACHE_CASE(8);
         RR_CACHE_CASE(9); RR_CACHE_CASE(10); RR_CACHE_CASE(11); RR_CACHE_CASE(12);

@@ -252,7 +252,9 @@ struct CacheEvictArgs {
 hipError_t launch_cache_evict(const CacheArgs& c, int dtype, const CacheEvictArgs& a, void* K, void* V, hipStream_t st);
 
 // (9) softmax weights that every key gets from the queries of a call: out[b][kv][key], fp32.
-hipError_t launch_key_weights(const Geom& g, int dtype, const void* Q, const void* K, const float* lse, float* out, hipStream_t st);
+size_t key_weights_bytes(const Geom& g, int dtype);         // 0: without a workspace
+hipError_t launch_key_weights(const Geom& g, int dtype, const void* Q, const void* K, const float* lse, float* out, void* workspace,
+                              hipStream_t st);
 
 // Raises a kernel's dynamic-LDS limit on the current device to at least `bytes`.  The limit is per (kernel,
 // device) and only ever grows, so the runtime is asked once per pair and size, not on every launch.

@@ -22,7 +22,9 @@ __device__ __forceinline__ void store_row4(bf16_t* p, const f32x4& v) {
     *reinterpret_cast<u32x2*>(p) = o;
 }
 
-template <typename T, int NT, int QT, int TL, int KW, int OCC>
+// D: d where it fills the matrix tiles, so that a row's last channels need no check (which would wait for the keys in front of
+// the work they are requested ahead of), or 0.
+template <typename T, int NT, int D, int QT, int TL, int KW, int OCC>
 __global__ void __launch_bounds__(64 * KW, OCC)
 k_window_generic(Geom g, WindowArgs a, float scale_log2, int tiles_q) {
     using F = Frag<T, NT, TL>;
@@ -32,7 +34,7 @@ k_window_generic(Geom g, WindowArgs a, float scale_log2, int tiles_q) {
     const float NEG_INF = -__builtin_huge_valf();
     const int t = threadIdx.x, lane = t & 63, x = lane & 15, gq = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int d = g.d;
+    const int d = D ? D : g.d;
 
     // heads fastest, and of those the KV head: the XCDs, which take consecutive workgroups in turn, each keep the keys of few
     // KV heads in L2; the last queries, which see most, first
@@ -212,25 +214,26 @@ hipError_t launch_window_generic(const Geom& g, int dtype, const WindowArgs& a, 
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * waves), 0, st, g, a, scale_log2, (int)tiles_q);
         return hipGetLastError();
     };
-    auto pick = [&](auto tiles) -> hipError_t {
-        constexpr int N = decltype(tiles)::value;
+    auto pick = [&](auto tiles, auto full) -> hipError_t {
+        constexpr int N = decltype(tiles)::value, D = decltype(full)::value;
         const long long rows = (long long)g.batch * g.Hq * g.Lq;
         if constexpr (N > 8) {
-            return dtype == RR_BF16 ? launch(k_window_generic<bf16_t, N, 1, 2, 4, 1>, 16, 4)
-                                    : launch(k_window_generic<float, N, 1, 1, 4, 1>, 16, 4);
+            return dtype == RR_BF16 ? launch(k_window_generic<bf16_t, N, D, 1, 2, 4, 1>, 16, 4)
+                                    : launch(k_window_generic<float, N, D, 1, 1, 4, 1>, 16, 4);
         } else {
             if (dtype == RR_BF16) {
                 if constexpr (N <= 4)
-                    if (rows >= 64 * 512) return launch(k_window_generic<bf16_t, N, 4, 2, 4, 2>, 64, 4);
-                return launch(k_window_generic<bf16_t, N, 2, 2, 4, 2>, 32, 4);
+                    if (rows >= 64 * 512) return launch(k_window_generic<bf16_t, N, D, 4, 2, 4, 2>, 64, 4);
+                return launch(k_window_generic<bf16_t, N, D, 2, 2, 4, 2>, 32, 4);
             }
-            if (rows >= 32 * 512) return launch(k_window_generic<float, N, 2, 1, 8, 2>, 32, 8);
-            return launch(k_window_generic<float, N, 1, 1, 8, 2>, 16, 8);
+            if (rows >= 32 * 512) return launch(k_window_generic<float, N, D, 2, 1, 8, 2>, 32, 8);
+            return launch(k_window_generic<float, N, D, 1, 1, 8, 2>, 16, 8);
         }
     };
     using std::integral_constant;
     switch ((g.d + 15) / 16) {
-#define RR_WINDOW_CASE(N) case N: return pick(integral_constant<int, N>{})
+#define RR_WINDOW_CASE(N) case N: return g.d == 16 * N ? pick(integral_constant<int, N>{}, integral_constant<int, 16 * N>{}) \
+                                                : pick(integral_constant<int, N>{}, integral_constant<int, 0>{})
         RR_WINDOW_CASE(1); RR_WINDOW_CASE(2); RR_WINDOW_CASE(3); RR_WINDOW_CASE(4);
         RR_WINDOW_CASE(5); RR_WINDOW_CASE(6); RR_WINDOW_CASE(7); RR_WINDOW_CASE(8);
         RR_WINDOW_CASE(9); RR_WINDOW_CASE(10); RR_WINDOW_CASE(11); RR_WINDOW_CASE(12);

@@ -134,8 +134,10 @@ def test_write_weights_and_evict_refusals():
     assert evict(sinks=60, recent=41) == bd.RR_ERR_PARAM and evict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1) == bd.RR_ERR_PARAM
     assert evict(width=1) == bd.RR_ERR_SHAPE and evict(width=0) == bd.RR_ERR_SHAPE and evict(s=shape(batch=70000)) == bd.RR_ERR_SHAPE
 
-    def weights(s=None, Q=FAKE, K=FAKE, lse=FAKE, out=FAKE):
-        return bd.lib.rr_key_weights(C.byref(s or shape()), Q, K, lse, out, None)
+    def weights(s=None, Q=FAKE, K=FAKE, lse=FAKE, out=FAKE, ws=FAKE * 16, n=1 << 40):
+        return bd.lib.rr_key_weights(C.byref(s or shape(Lq=512)), Q, K, lse, out, ws, n, None)
+    assert bd.lib.rr_key_weights_workspace_bytes(C.byref(shape(Lq=512))) > 0 == bd.lib.rr_key_weights_workspace_bytes(C.byref(shape(Lq=1)))
+    assert weights(ws=None) == bd.RR_ERR_WORKSPACE and weights(n=64) == bd.RR_ERR_WORKSPACE and weights(ws=FAKE * 16 + 16) == bd.RR_ERR_WORKSPACE
     assert weights(Q=None) == bd.RR_ERR_NULL and weights(lse=None) == bd.RR_ERR_NULL and weights(out=None) == bd.RR_ERR_NULL
     assert weights(K=FAKE + 2) == bd.RR_ERR_SHAPE and weights(s=shape(batch=70000)) == bd.RR_ERR_SHAPE
 
