@@ -128,7 +128,8 @@ RR_API int rr_window_attn(const rr_shape* shape, const void* Q, const void* K, c
         e = launch_cache_attn(c, shape->dtype, plan, (hipStream_t)hip_stream);
     } else {
         const WindowArgs a = {Q, K, V, O, lse, std::min(window, g.L), std::min(sinks, g.L), seq_first, B};
-        e = launch_window_generic(g, shape->dtype, a, (hipStream_t)hip_stream);
+        e = window_mfma_takes(g, shape->dtype, seq_first, B) ? launch_window_mfma(g, a, (hipStream_t)hip_stream)
+                                                             : launch_window_generic(g, shape->dtype, a, (hipStream_t)hip_stream);
     }
     return e == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
 }

@@ -139,7 +139,9 @@ __device__ __forceinline__ void pv_step(Wave& w, int buf, int t, const bf16x8 (&
     mfma_settle_acc(w.acc);
 }
 
-// P of a step's 16 scores against a reference: exp2, rounded; the sum of the rounded terms and of what rounding took.
+// P of a step's 16 scores against a reference: exp2, rounded; the sum of the rounded terms and of what rounding took.  (kExact,
+// here and below: the sum of the terms before rounding, and nothing taken.)
+template <bool kExact = false>
 __device__ __forceinline__ void exp_all(const Wave& w, const f32x16& s, float ref, bf16x8 (&p)[2], float& psum, float& fix) {
     const float nb = -ref;
     bf16x2 ones;
@@ -160,7 +162,8 @@ __device__ __forceinline__ void exp_all(const Wave& w, const f32x16& s, float re
         p[r >> 3][(r & 7) + 1] = pr[1];
         psum = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, psum, false);
     }
-    fix = sum - psum;
+    if (kExact) psum = sum;
+    fix = kExact ? 0.f : sum - psum;
 }
 __device__ __forceinline__ float max_of(const f32x16& s) {
     float mx = -__builtin_huge_valf();
@@ -173,6 +176,7 @@ __device__ __forceinline__ float max_of(const f32x16& s) {
 // denominator, and recomputes P of the step at hand.  Rare; entered by the whole wave.  (Where registers are short, each
 // tile of O^T is back in place before the next is taken; without that the ragged and persistent forms spill 12 to 25
 // registers: 32K tokens 3357 against 3296 us.  The plain form has room, and is 0.7 % faster without: 64K, 64 heads.)
+template <bool kExact = false>
 __device__ __forceinline__ void move_reference(Wave& w, const f32x16& s, bf16x8 (&p)[2], float& psum, float& fix, float mx) {
     mfma_settle_acc(w.acc);                             // O^T is about to be read by vector instructions
     float top = mx * w.sl2;
@@ -189,16 +193,17 @@ __device__ __forceinline__ void move_reference(Wave& w, const f32x16& s, bf16x8 
         for (int r = 0; r < 16; ++r) w.acc[dt][r] *= alpha;
         if (w.tight) asm volatile("" : "+a"(w.acc[dt]));
     }
-    exp_all(w, s, use, p, psum, fix);
+    exp_all<kExact>(w, s, use, p, psum, fix);
     mfma_settle_acc(w.acc);                             // ... and was written by them
 }
 
 // softmax of one 32-key step, nothing overlapped (the diagonal block)
+template <bool kExact = false>
 __device__ __forceinline__ void softmax_step(Wave& w, const f32x16& s, bf16x8 (&p)[2]) {
     float psum, fix;
-    exp_all(w, s, w.mref, p, psum, fix);
+    exp_all<kExact>(w, s, w.mref, p, psum, fix);
     const float mx = max_of(s);
-    if (__any(mx * w.sl2 > w.mref + w.lazy)) move_reference(w, s, p, psum, fix, mx);
+    if (__any(mx * w.sl2 > w.mref + w.lazy)) move_reference<kExact>(w, s, p, psum, fix, mx);
     w.lsum += psum;
     w.lfix += fix;
 }
@@ -278,7 +283,7 @@ __device__ __forceinline__ void wait_vm() { asm volatile("s_waitcnt vmcnt(0)" ::
 // with the wave's global -> LDS copies of the prefetched K and V tiles, one every other slot, so the
 // copies never queue up in front of the arithmetic.  `valid` is false for the two fill phases at either end of a
 // row, whose softmax is thrown away.
-template <bool kFetch, int VOFF, int KOFF>
+template <bool kFetch, int VOFF, int KOFF, bool kExact = false>
 __device__ __forceinline__ void phase(Wave& w, const f32x16& scur, f32x16& snext,
                                       const bf16x8 (&pprev)[2], bf16x8 (&pcur)[2],
                                       bool valid, const Stager& st,
@@ -321,10 +326,15 @@ __device__ __forceinline__ void phase(Wave& w, const f32x16& scur, f32x16& snext
         }
         if (sidx >= 4 && !(sidx & 1) && (sidx - 4) / 2 < NE / 2) {  // D
             const int er = sidx - 4;
-            bf16x2 pr;
-            pr[0] = pcur[er >> 3][er & 7];
-            pr[1] = pcur[er >> 3][(er & 7) + 1];
-            psum = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, psum, false);   // sums what PV will use
+            if (kExact) {
+                psum += ev[er];
+                psum += ev[er + 1];
+            } else {
+                bf16x2 pr;
+                pr[0] = pcur[er >> 3][er & 7];
+                pr[1] = pcur[er >> 3][(er & 7) + 1];
+                psum = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, psum, false);   // sums what PV will use
+            }
             asm volatile("" : "+v"(psum));
         }
     };
@@ -370,7 +380,7 @@ __device__ __forceinline__ void phase(Wave& w, const f32x16& scur, f32x16& snext
     if (valid) {
         if (__any(!(psum <= w.lazy_sum))) {
             float fix;
-            move_reference(w, scur, pcur, psum, fix, max_of(scur));
+            move_reference<kExact>(w, scur, pcur, psum, fix, max_of(scur));
             w.lfix += fix;
         }
         w.lsum += psum;

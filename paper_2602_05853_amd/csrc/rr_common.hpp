@@ -202,6 +202,8 @@ struct WindowArgs {
     const int32_t* seq_first;   // packed sequences, as in AttnArgs; nullptr = one sequence
     int B;
 };
+bool window_mfma_takes(const Geom& g, int dtype, const int32_t* seq_first, int B);   // bf16, d = 128
+hipError_t launch_window_mfma(const Geom& g, const WindowArgs& a, hipStream_t st);
 hipError_t launch_window_generic(const Geom& g, int dtype, const WindowArgs& a, hipStream_t st);
 
 // (6) a key-value cache in pages, or the contiguous keys and values of a step (table and length nullptr, page 0).
