@@ -330,9 +330,10 @@ int rr_dense_attn_ws(const rr_shape* shape, const void* Q, const void* K, const 
  *   lse        optional, as for rr_sparse_attn.
  *   workspace  NULL, or at least rr_window_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards: steps of at
  *              most 16 positions and 32 query rows per KV head then share the keys of a KV head out among several workgroups
- *              and read them once for all its query heads.  rr_window_workspace_bytes() is 0 for every other call.
+ *              and read them once for all its query heads.  rr_window_workspace_bytes() is 0 for every other call, and for such
+ *              steps that see few keys, which run that way without one.
  * Any L, d and strides of the conventions above.  bf16 with d = 128 (packed: B = 128) runs on a kernel of its own, which rounds
- * the probabilities to bf16; steps with a workspace and all other shapes hold nothing in fewer than 32 bits.  An infinite
+ * the probabilities to bf16; such steps and all other shapes hold nothing in fewer than 32 bits.  An infinite
  * or NaN value of V that no query of a launch's tile sees does not reach it; one that a query in the same tile sees makes the
  * channel NaN in that tile's other rows, as zero times infinity does.
  */
@@ -346,7 +347,7 @@ int rr_window_attn(const rr_shape* shape, const void* Q, const void* K, const vo
  * sequence b lies in page table[b][p / page] at slot p % page.  K and V are pools of pages addressed as
  * base + page*kv_stride_b + h*kv_stride_h + slot*kv_stride_l + c with the strides of the rr_shape of the call (so both
  * [pages, Hkv, page, d] and [pages, page, Hkv, d] are possible).
- *   weight     [num_pages, Hkv, page] fp32 contiguous: what every position's key has got of softmax weights so far.  May be NULL
+ *   weight     [num_pages, Hkv, page] fp32 contiguous, 16-byte aligned: what every position's key has got of softmax weights so far.  May be NULL
  *              where nothing reads or writes it.
  *   table      [batch, width] int32.  An entry outside [0, num_pages) is no page: its positions hold nothing, are attended by
  *              nobody and are not written.
@@ -391,7 +392,7 @@ int rr_paged_write(const rr_shape* shape, const rr_paged_cache* cache, const voi
  *              Lq rows of the KV head's query heads, cache->weight[page][kv][slot] += sum_rows exp(q k / sqrt(d) - lse).
  *   lse        optional [batch, Hq, Lq].
  *   workspace  rr_paged_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards.  (The cache's arrays may be
- *              NULL there; page, num_pages and width are used.)  0 on an invalid geometry.
+ *              NULL there; page, num_pages and width are used.)  0 where none is needed, and on an invalid geometry.
  * The blocks of all sequences are shared out evenly among the workgroups of one launch, whatever the lengths; parts are fp32 and
  * joined in a fixed order, so equal calls give equal bits.  O is rounded once.
  */

@@ -18,10 +18,16 @@ _NAMES = ("BlockMask", "RRError", "rr_dense_attn", "rr_estimate", "rr_sparse_att
           "rr_key_weights", "rr_key_weights_workspace_bytes", "rr_cache_evict",
           "RR_FLAG_PROTECT_LAST", "RR_FLAG_DIAGONAL_TOKEN", "LIB_PATH", "OFFSET_MODES")
 
+# (a reload looks them up again)
+for _name in _NAMES + ("binding",):
+    globals().pop(_name, None)
+
 
 def __getattr__(name):
     if name in _NAMES or name == "binding":
         import importlib
         binding = importlib.import_module(".binding", __name__)
-        return binding if name == "binding" else getattr(binding, name)
+        value = binding if name == "binding" else getattr(binding, name)
+        globals()[name] = value          # the next use finds it without this function (1.x us)
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -433,22 +433,34 @@ def rr_mask_from_dense(Q: torch.Tensor, K: torch.Tensor, dense: torch.Tensor, B:
 
 # ---- window attention, the paged cache, key weights (see the header for what each computes) ----
 
-def _on_device(device: torch.device, *tensors) -> None:
-    """Every tensor of a call lies on the one GPU the call runs on."""
-    if device.type != "cuda":
+# The host's share of a short call: checks are plain comparisons of what torch hands out as it is (a device by its index, sizes as
+# torch.Size), the cache's struct is made once and again when one of its tensors is replaced or moves (one token for four short
+# sequences 13.8 -> 6.x us of Python, a step's write 12.6 -> 6.x).
+
+def _on_device(index: int, *tensors) -> None:
+    """Every tensor of a call lies on the one GPU the call runs on (-1: the CPU)."""
+    if index < 0:
         raise RRError(RR_ERR_PARAM)
     for t in tensors:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != index:
             raise RRError(RR_ERR_PARAM)
 
 
-def _call(device: torch.device, stream: Optional[torch.cuda.Stream], entry, *args) -> None:
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _call(index: int, stream: Optional[torch.cuda.Stream], entry, *args) -> None:
     """entry(*args, stream) with the tensors' device current."""
-    if device.index == torch.cuda.current_device():
-        _check(entry(*args, _stream_ptr(stream)))
+    if index == torch.cuda.current_device():
+        if stream is not None:
+            status = entry(*args, stream.cuda_stream)
+        else:
+            status = entry(*args, _raw_stream(index) if _raw_stream is not None else _stream_ptr(None))
     else:
-        with torch.cuda.device(device):
-            _check(entry(*args, _stream_ptr(stream)))
+        with torch.cuda.device(index):
+            status = entry(*args, _stream_ptr(stream))
+    if status != RR_OK:
+        raise RRError(status)
 
 
 def _check_like(t: torch.Tensor, like: torch.Tensor) -> None:
@@ -457,9 +469,9 @@ def _check_like(t: torch.Tensor, like: torch.Tensor) -> None:
 
 
 def _check_array(t: torch.Tensor, dtype: torch.dtype, shape) -> None:
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise RRError(RR_ERR_DTYPE)
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise RRError(RR_ERR_SHAPE)
 
 
@@ -497,8 +509,9 @@ def rr_window_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, window: in
         if B < 1:
             raise RRError(RR_ERR_SHAPE)
         _check_seq_first(seq_first, _blocks(shp.L, B), Q.device)
-    _on_device(Q.device, K, V, O, lse, workspace)
-    _call(Q.device, stream, lib.rr_window_attn, C.byref(shp), Q.data_ptr(), K.data_ptr(), V.data_ptr(), window, sinks,
+    index = Q.get_device()
+    _on_device(index, K, V, O, lse, workspace)
+    _call(index, stream, lib.rr_window_attn, C.byref(shp), Q.data_ptr(), K.data_ptr(), V.data_ptr(), window, sinks,
           _ptr(seq_first), B, O.data_ptr(), _ptr(lse), _ptr(workspace), _bytes(workspace))
     return O
 
@@ -526,8 +539,17 @@ class PagedCache:
                           torch.zeros(batch, dtype=torch.int32, device=device),
                           torch.zeros(pages, Hkv, page, dtype=torch.float32, device=device) if weight else None)
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_made", None)          # the struct is of other tensors
+
     def c_struct(self) -> rr_paged_cache:
-        K, V, table = self.K, self.V, self.table
+        """The cache's struct, its tensors checked against each other; kept until one of them is replaced or has moved."""
+        K, V, table, length, weight = self.K, self.V, self.table, self.length, self.weight
+        at = (K.data_ptr(), V.data_ptr(), weight.data_ptr() if weight is not None else None, table.data_ptr(), length.data_ptr())
+        made = self._made
+        if made is not None and made[0] == at:
+            return made[1]
         if K.dim() != 4 or table.dim() != 2 or K.stride(3) != 1 or V.stride() != K.stride() or V.shape != K.shape:
             raise RRError(RR_ERR_SHAPE)
         if V.dtype != K.dtype:
@@ -535,29 +557,33 @@ class PagedCache:
         pages, Hkv, page, _ = K.shape
         batch, width = table.shape
         _check_array(table, torch.int32, (batch, width))
-        _check_array(self.length, torch.int32, (batch,))
-        if self.weight is not None:
-            _check_array(self.weight, torch.float32, (pages, Hkv, page))
-        return rr_paged_cache(K.data_ptr(), V.data_ptr(), _ptr(self.weight), table.data_ptr(), self.length.data_ptr(), page, pages,
-                              width)
+        _check_array(length, torch.int32, (batch,))
+        if weight is not None:
+            _check_array(weight, torch.float32, (pages, Hkv, page))
+        for t in (V, table, length, weight):
+            if t is not None and t.device != K.device:
+                raise RRError(RR_ERR_PARAM)
+        struct = rr_paged_cache(*at, page, pages, width)
+        object.__setattr__(self, "_made", (at, struct))
+        return struct
 
     def shape(self, rows: torch.Tensor, Hq: int, max_length: Optional[int]) -> rr_shape:
         """The rr_shape of a call whose query (or new) rows are `rows` [batch, heads, Lq, d]."""
         K = self.K
-        if rows.dim() != 4 or rows.stride(3) != 1 or rows.shape[0] != self.table.shape[0] or rows.shape[3] != K.shape[3] or \
-                rows.shape[2] < 1:
+        r, k, of_rows, of_pool = rows.stride(), K.stride(), rows.shape, K.shape
+        batch, width = self.table.shape
+        if len(of_rows) != 4 or r[3] != 1 or of_rows[0] != batch or of_rows[3] != of_pool[3] or of_rows[2] < 1:
             raise RRError(RR_ERR_SHAPE)
-        if rows.dtype != K.dtype:
+        if rows.dtype is not K.dtype:
             raise RRError(RR_ERR_DTYPE)
-        r, k = rows.stride(), K.stride()
-        L = self.table.shape[1] * K.shape[2] if max_length is None else max_length
-        return rr_shape(rows.shape[0], L, Hq, K.shape[1], K.shape[3], _dtype_code(K), r[0], r[1], r[2], k[0], k[1], k[2],
-                        rows.shape[2])
+        return rr_shape(batch, width * of_pool[2] if max_length is None else max_length, Hq, of_pool[1], of_pool[3], _dtype_code(K),
+                        r[0], r[1], r[2], k[0], k[1], k[2], of_rows[2])
 
 
 def rr_paged_workspace_bytes(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: int = 0, accumulate: bool = False,
                              max_length: Optional[int] = None) -> int:
-    shp, c = cache.shape(Q, Q.shape[1], max_length), cache.c_struct()
+    c = cache.c_struct()
+    shp = cache.shape(Q, Q.shape[1], max_length)
     return lib.rr_paged_workspace_bytes(C.byref(shp), C.byref(c), window, sinks, RR_FLAG_ACCUMULATE if accumulate else 0)
 
 
@@ -566,7 +592,8 @@ def rr_paged_attn(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: in
                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Attention of the last Lq positions of every sequence, Q [batch, Hq, Lq, d], against the cache.  max_length: the most
     positions a sequence has (default: what the table holds).  Without `workspace` one is allocated."""
-    shp, c = cache.shape(Q, Q.shape[1], max_length), cache.c_struct()
+    c = cache.c_struct()
+    shp = cache.shape(Q, Q.shape[1], max_length)
     flags = RR_FLAG_ACCUMULATE if accumulate else 0
     if O is None:
         O = _output_like(Q)
@@ -574,11 +601,12 @@ def rr_paged_attn(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: in
         _check_like(O, Q)
     if lse is not None:
         _check_array(lse, torch.float32, Q.shape[:3])
-    _on_device(Q.device, cache.K, cache.V, cache.table, cache.length, cache.weight, O, lse, workspace)
+    index = Q.get_device()
+    _on_device(index, cache.K, O, lse, workspace)
     if workspace is None:
         workspace = torch.empty(lib.rr_paged_workspace_bytes(C.byref(shp), C.byref(c), window, sinks, flags), dtype=torch.uint8,
                                 device=Q.device)
-    _call(Q.device, stream, lib.rr_paged_attn, C.byref(shp), Q.data_ptr(), C.byref(c), window, sinks, flags, O.data_ptr(), _ptr(lse),
+    _call(index, stream, lib.rr_paged_attn, C.byref(shp), Q.data_ptr(), C.byref(c), window, sinks, flags, O.data_ptr(), _ptr(lse),
           workspace.data_ptr(), _bytes(workspace))
     return O
 
@@ -588,17 +616,19 @@ def rr_paged_write(cache: PagedCache, K: torch.Tensor, V: torch.Tensor, count: O
     """The last count[b] (default: all Lq) of the sequences' positions into their pages, from K, V [batch, Hkv, Lq, d]; set
     cache.length to include them first."""
     Hkv = cache.K.shape[1]
-    shp, c = cache.shape(K, Hkv, None), cache.c_struct()
+    c = cache.c_struct()
+    shp = cache.shape(K, Hkv, None)
     if K.shape[1] != Hkv or V.shape != K.shape or V.stride() != K.stride():
         raise RRError(RR_ERR_SHAPE)
-    if V.dtype != K.dtype:
+    if V.dtype is not K.dtype:
         raise RRError(RR_ERR_DTYPE)
     if count is not None:
-        _check_array(count, torch.int32, (K.shape[0],))
+        _check_array(count, torch.int32, K.shape[:1])
     if weight is not None:
         _check_array(weight, torch.float32, K.shape[:3])
-    _on_device(K.device, V, count, weight, cache.K, cache.V, cache.table, cache.length, cache.weight)
-    _call(K.device, stream, lib.rr_paged_write, C.byref(shp), C.byref(c), K.data_ptr(), V.data_ptr(), _ptr(count), _ptr(weight))
+    index = K.get_device()
+    _on_device(index, V, count, weight, cache.K)
+    _call(index, stream, lib.rr_paged_write, C.byref(shp), C.byref(c), K.data_ptr(), V.data_ptr(), _ptr(count), _ptr(weight))
 
 
 def rr_key_weights_workspace_bytes(Q: torch.Tensor, K: torch.Tensor) -> int:
@@ -618,11 +648,12 @@ def rr_key_weights(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, out: Opt
         out = torch.empty(K.shape[:3], dtype=torch.float32, device=K.device)
     else:
         _check_array(out, torch.float32, K.shape[:3])
-    _on_device(Q.device, K, lse, out, workspace)
+    index = Q.get_device()
+    _on_device(index, K, lse, out, workspace)
     if workspace is None:
         n = lib.rr_key_weights_workspace_bytes(C.byref(shp))
         workspace = torch.empty(n, dtype=torch.uint8, device=Q.device) if n else None
-    _call(Q.device, stream, lib.rr_key_weights, C.byref(shp), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), out.data_ptr(),
+    _call(index, stream, lib.rr_key_weights, C.byref(shp), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), out.data_ptr(),
           _ptr(workspace), _bytes(workspace))
     return out
 
@@ -633,22 +664,26 @@ def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int
     """Holds every sequence to `keep` positions by accumulated weight, head by head, into the pages of `table` [batch, width]
     (of the same pools, none of them in use).  Returns the cache over those pages and the kept source positions [batch, Hkv,
     keep] (-1 behind the last)."""
-    shp, c = cache.shape(cache.K[:1].expand(cache.table.shape[0], -1, -1, -1), cache.K.shape[1], None), cache.c_struct()
-    batch, Hkv = shp.batch, shp.Hkv
+    c = cache.c_struct()
+    K = cache.K
+    (batch, width), (_, Hkv, page, d), k = cache.table.shape, K.shape, K.stride()
+    # (no rows of queries belong to the call: the pool's own layout in their place)
+    shp = rr_shape(batch, width * page, Hkv, Hkv, d, _dtype_code(K), k[0], k[1], k[2], k[0], k[1], k[2], 1)
     if keep < 1:
         raise RRError(RR_ERR_PARAM)
     if table.dim() != 2:
         raise RRError(RR_ERR_SHAPE)
     _check_array(table, torch.int32, (batch, table.shape[1]))
     if length is None:
-        length = torch.empty(batch, dtype=torch.int32, device=cache.K.device)
+        length = torch.empty(batch, dtype=torch.int32, device=K.device)
     else:
         _check_array(length, torch.int32, (batch,))
     if kept is None:
-        kept = torch.empty((batch, Hkv, keep), dtype=torch.int32, device=cache.K.device)
+        kept = torch.empty((batch, Hkv, keep), dtype=torch.int32, device=K.device)
     else:
         _check_array(kept, torch.int32, (batch, Hkv, keep))
-    _on_device(cache.K.device, cache.V, cache.table, cache.length, cache.weight, table, length, kept)
-    _call(cache.K.device, stream, lib.rr_cache_evict, C.byref(shp), C.byref(c), keep, sinks, recent, table.data_ptr(), table.shape[1],
+    index = K.get_device()
+    _on_device(index, table, length, kept)
+    _call(index, stream, lib.rr_cache_evict, C.byref(shp), C.byref(c), keep, sinks, recent, table.data_ptr(), table.shape[1],
           length.data_ptr(), kept.data_ptr())
     return PagedCache(cache.K, cache.V, table, length, cache.weight), kept

@@ -47,6 +47,7 @@ bool window_step(const Geom& g, int dtype, int window, int sinks, CacheArgs* c, 
     c->scale_log2 = (float)(1.4426950408889634 / sqrt((double)g.d));
     if (!cache_attn_plan(*c, dtype, false, plan)) return false;
     c->row_tiles = plan->row_tiles;
+    c->whole = plan->whole;
     return true;
 }
 
@@ -121,8 +122,8 @@ RR_API int rr_window_attn(const rr_shape* shape, const void* Q, const void* K, c
     CacheArgs c;
     CachePlan plan;
     hipError_t e;
-    if (workspace && !seq_first && window_step(g, shape->dtype, window, sinks, &c, &plan)) {
-        if (workspace_bytes < plan.total() || misaligned256(workspace)) return RR_ERR_WORKSPACE;
+    if (!seq_first && window_step(g, shape->dtype, window, sinks, &c, &plan) && (workspace || plan.total() == 0)) {
+        if (plan.total() && (workspace_bytes < plan.total() || misaligned256(workspace))) return RR_ERR_WORKSPACE;
         c.Q = Q; c.K = K; c.V = V; c.O = O; c.lse = lse;
         set_workspace(&c, plan, workspace);
         e = launch_cache_attn(c, shape->dtype, plan, (hipStream_t)hip_stream);
@@ -151,14 +152,16 @@ RR_API int rr_paged_attn(const rr_shape* shape, const void* Q, const rr_paged_ca
     if (flags & ~RR_FLAG_ACCUMULATE) return RR_ERR_PARAM;
     const bool accumulate = (flags & RR_FLAG_ACCUMULATE) != 0;
     if (accumulate && !cache->weight) return RR_ERR_NULL;
+    if (accumulate && !aligned16(cache->weight)) return RR_ERR_SHAPE;
     if (!aligned16(Q) || !aligned16(O) || !outputs_distinct(shape, c.T)) return RR_ERR_SHAPE;
     rc = set_window(&c, window, sinks);
     if (rc != RR_OK) return rc;
     CachePlan plan;
     if (!cache_attn_plan(c, shape->dtype, accumulate, &plan)) return RR_ERR_SHAPE;
-    if (!workspace || workspace_bytes < plan.total() || misaligned256(workspace)) return RR_ERR_WORKSPACE;
+    if (plan.total() && (!workspace || workspace_bytes < plan.total() || misaligned256(workspace))) return RR_ERR_WORKSPACE;
     c.Q = Q; c.O = O; c.lse = lse;
     c.row_tiles = plan.row_tiles;
+    c.whole = plan.whole;
     set_workspace(&c, plan, workspace);
     return launch_cache_attn(c, shape->dtype, plan, (hipStream_t)hip_stream) == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
 }

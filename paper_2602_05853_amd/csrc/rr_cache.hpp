@@ -50,47 +50,62 @@ __device__ __forceinline__ Visit visit(const CacheArgs& c, int b) { return visit
 // of W takes units U w / W .. U (w + 1) / W - 1, whatever sequences they belong to, so all end together however uneven the
 // lengths are; the part of a pair that a workgroup computes has slot w + (number of the pair), which is its own: from one
 // part to the next at least one of the two grows.
-// Every workgroup adds the lengths up for itself: thread t the sequences t per .. t per + per - 1, then a scan over threads.
+// Every workgroup adds the lengths up for itself: up to 64 sequences a lane each, in every wave (no LDS, no barrier); more, thread t
+// the sequences t per .. t per + per - 1, then a scan over threads.
 template <int kThreads> struct Shares {
     int pre[kThreads + 1];                      // blocks of the sequences in front of thread t's
     int wave[kThreads / 64];
     int at;
 };
-template <int kThreads>
-__device__ __forceinline__ int shares_scan(const CacheArgs& c, Shares<kThreads>& s) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int per = (c.batch + kThreads - 1) / kThreads;
-    int own = 0;
-    for (int i = 0; i < per; ++i) {
-        const int b = tid * per + i;
-        if (b < c.batch) {
-            int n = c.L;
-            if (c.length) {
-                n = c.length[b];
-                n = n < 0 ? 0 : (n > c.L ? c.L : n);
-            }
-            own += visit_of(n, c.T, c.window, c.sinks).n;
-        }
+__device__ __forceinline__ int blocks_of(const CacheArgs& c, int b) {
+    int n = c.L;
+    if (c.length) {
+        n = c.length[b];
+        n = n < 0 ? 0 : (n > c.L ? c.L : n);
     }
-    int sum = own;
+    return visit_of(n, c.T, c.window, c.sinks).n;
+}
+__device__ __forceinline__ int scan_lanes(int v) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(sum, o);
-        if (lane >= o) sum += up;
+        const int up = __shfl_up(v, o);
+        if (lane >= o) v += up;
     }
-    if (lane == 63) s.wave[w] = sum;
+    return v;
+}
+// Blocks of all sequences; `upto`: of those up to the lane's (up to 64 sequences).
+template <int kThreads>
+__device__ __forceinline__ int shares_scan(const CacheArgs& c, Shares<kThreads>& s, int& upto) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (c.batch <= 64) {
+        upto = scan_lanes(lane < c.batch ? blocks_of(c, lane) : 0);
+        return __builtin_amdgcn_readlane(upto, 63);
+    }
+    const int per = (c.batch + kThreads - 1) / kThreads;
+    int own = 0;
+    for (int i = 0; i < per; ++i)
+        if (tid * per + i < c.batch) own += blocks_of(c, tid * per + i);
+    upto = scan_lanes(own);
+    if (lane == 63) s.wave[w] = upto;
     __syncthreads();
     int front = 0;
 #pragma unroll
     for (int i = 0; i < kThreads / 64; ++i) front += i < w ? s.wave[i] : 0;
-    s.pre[tid] = front + sum - own;
-    if (tid == kThreads - 1) s.pre[kThreads] = front + sum;
+    s.pre[tid] = front + upto - own;
+    if (tid == kThreads - 1) s.pre[kThreads] = front + upto;
     __syncthreads();
     return s.pre[kThreads];
 }
 // The sequence that block `at` (0 <= at < the scan's total) of all sequences belongs to, its first block and its visit.
 template <int kThreads>
-__device__ __forceinline__ int shares_find(const CacheArgs& c, Shares<kThreads>& s, int at, int* base, Visit* v) {
+__device__ __forceinline__ int shares_find(const CacheArgs& c, Shares<kThreads>& s, int upto, int at, int* base, Visit* v) {
+    if (c.batch <= 64) {
+        const int b = __popcll(__ballot(upto <= at));
+        *base = b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+        *v = visit(c, b);
+        return b;
+    }
     const int tid = threadIdx.x;
     if (s.pre[tid] <= at && at < s.pre[tid + 1]) s.at = tid;
     __syncthreads();
@@ -102,9 +117,17 @@ __device__ __forceinline__ int shares_find(const CacheArgs& c, Shares<kThreads>&
         front += v->n;
         *v = visit(c, ++b);
     }
-    __syncthreads();                            // s.at may be written again
     *base = front;
     return b;
+}
+// Blocks of the sequences in front of sequence b
+template <int kThreads>
+__device__ __forceinline__ int shares_front(const CacheArgs& c, const Shares<kThreads>& s, int upto, int b) {
+    if (c.batch <= 64) return b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
+    const int per = (c.batch + kThreads - 1) / kThreads;
+    int front = s.pre[b / per];
+    for (int i = b / per * per; i < b; ++i) front += visit(c, i).n;
+    return front;
 }
 // Workgroups that take part in U units
 __device__ __forceinline__ long long shares_count(long long U, int workgroups) {

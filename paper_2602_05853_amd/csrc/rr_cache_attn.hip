@@ -24,6 +24,14 @@ namespace rr {
 namespace {
 
 constexpr int kCacheWorkgroups = 512;                   // two per compute unit, all resident
+constexpr int kWholeBlocks = 4;                         // sequences that visit at most so many are not shared out
+
+__device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t* p, const f32x4& v) {
+    const u32x2 o = {f32_to_bf16_bits(v[0]) | (f32_to_bf16_bits(v[1]) << 16),
+                     f32_to_bf16_bits(v[2]) | (f32_to_bf16_bits(v[3]) << 16)};
+    *reinterpret_cast<u32x2*>(p) = o;
+}
 
 // D: d where it fills the matrix tiles, so that a row's last channels need no check (which would wait for the keys in front of
 // the work they are requested ahead of), or 0.
@@ -44,15 +52,29 @@ k_cache_attn(CacheArgs c) {
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = c.G * c.T, pairs = c.Hkv * c.row_tiles;
 
-    const int total = shares_scan(c, s_shares);
-    const long long U = (long long)total * pairs, W = shares_count(U, (int)gridDim.x);
-    if ((long long)blockIdx.x >= W) return;
-    long long u = U * blockIdx.x / W;
-    const long long u_end = U * (blockIdx.x + 1) / W;
-    int base;
+    long long u, u_end;
     Visit v;
-    int b = shares_find(c, s_shares, (int)(u / pairs), &base, &v);
-    int pair = (int)((u - (long long)base * pairs) / v.n), i_lo = (int)(u - (long long)base * pairs - (long long)pair * v.n);
+    int b, pair, i_lo;
+    if (c.whole) {
+        // a workgroup to a sequence and pair, which stores its rows itself (their units are numbered as if all sequences visited as
+        // many blocks as any may)
+        b = (int)blockIdx.x / pairs;
+        pair = (int)blockIdx.x - b * pairs;
+        i_lo = 0;
+        v = visit(c, b);
+        u = (long long)blockIdx.x * c.whole;
+        u_end = u + v.n;
+    } else {
+        int upto, base;
+        const int total = shares_scan(c, s_shares, upto);
+        const long long U = (long long)total * pairs, W = shares_count(U, (int)gridDim.x);
+        if ((long long)blockIdx.x >= W) return;
+        u = U * blockIdx.x / W;
+        u_end = U * (blockIdx.x + 1) / W;
+        b = shares_find(c, s_shares, upto, (int)(u / pairs), &base, &v);
+        pair = (int)((u - (long long)base * pairs) / v.n);
+        i_lo = (int)(u - (long long)base * pairs - (long long)pair * v.n);
+    }
 
     // rows of a tile this lane reads, relative to its first key
     const long long k_off = (long long)x * c.ksl;
@@ -60,7 +82,7 @@ k_cache_attn(CacheArgs c) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) v_off[r] = (long long)(4 * gq + r) * c.ksl;
 
-    while (u < u_end) {
+    do {
         const int blocks = (int)min((long long)(v.n - i_lo), u_end - u);
         const int kv = pair / c.row_tiles, rt = pair - kv * c.row_tiles;
         const int q_first = v.len - c.T, q_last = v.len - 1;
@@ -113,9 +135,11 @@ k_cache_attn(CacheArgs c) {
 #pragma unroll
                 for (int ch = 0; ch < NT; ++ch) acc[t][ch] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
-            request(0);
-            load_keys(0);
-            request(min(1, steps - 1));
+            if (steps > 0) {
+                request(0);
+                load_keys(0);
+                request(min(1, steps - 1));
+            }
             for (int st = 0; st < steps; ++st) {
                 typename F::V vf;
 #pragma unroll
@@ -216,8 +240,18 @@ k_cache_attn(CacheArgs c) {
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = l > 0.f ? o[e] / l : 0.f;
-            *reinterpret_cast<f32x4*>(c.part_O + (slot * kQ + q) * d + ch) = o;
-            if (ch == 0) c.part_lse[slot * kQ + q] = l > 0.f ? top + log2f(l) : NEG_INF;
+            if (!c.whole) {
+                *reinterpret_cast<f32x4*>(c.part_O + (slot * kQ + q) * d + ch) = o;
+                if (ch == 0) c.part_lse[slot * kQ + q] = l > 0.f ? top + log2f(l) : NEG_INF;
+            } else {
+                const int rr = kQ * rt + q, hl = rr / c.T, tk = rr - hl * c.T, h = kv * c.G + hl;
+                store4(reinterpret_cast<T*>(c.O) + b * c.qsb + h * c.qsh + tk * c.qsl + ch, o);
+                if (ch == 0) {
+                    const float l2 = top + log2f(l);
+                    if (c.lse) c.lse[((long long)b * c.Hq + h) * c.T + tk] = l > 0.f ? l2 * 0.6931471805599453f : NEG_INF;
+                    if (c.row_lse) c.row_lse[((long long)b * c.Hkv + kv) * R + rr] = l > 0.f ? l2 : -NEG_INF;
+                }
+            }
         }
         __syncthreads();                                 // the shares' places are free again
 
@@ -230,35 +264,33 @@ k_cache_attn(CacheArgs c) {
                 do v = visit(c, ++b); while (v.n == 0);  // (units are left, so a sequence that has some follows)
             }
         }
-    }
+    } while (u < u_end);
 }
 
 // One workgroup per query row: O = sum_p w_p O_p / sum_p w_p with w_p = 2^(lse_p - max), rounded once.
+// A wave takes every fourth part, eight requested at once: one at a time their latencies were the kernel (64 parts 15 us).
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_cache_join(CacheArgs c, int row_tile, int workgroups) {
     __shared__ Shares<256> s_shares;
     __shared__ float s_w[kCacheWorkgroups];
-    __shared__ float s_red[4];
-    __shared__ float s_o[4][256];
+    __shared__ float s_red[4], s_den[4];
+    __shared__ __align__(16) float s_o[4][256];
     const float NEG_INF = -__builtin_huge_valf();
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int R = c.G * c.T, pairs = c.Hkv * c.row_tiles;
-    int row = blockIdx.x;                                // (b, kv, r)
+    const int row = blockIdx.x;                          // (b, kv, r)
     const int r = row % R, kv = row / R % c.Hkv, b = row / R / c.Hkv;
     const int pair = kv * c.row_tiles + r / row_tile;
 
-    const int total = shares_scan(c, s_shares);
+    int upto;
+    const int total = shares_scan(c, s_shares, upto);
     const long long U = (long long)total * pairs, W = shares_count(U, workgroups);
     const Visit v = visit(c, b);
     int parts = 0;
     long long first = 0;
     if (v.n > 0) {
-        // blocks in front of sequence b
-        const int per = (c.batch + 255) / 256;
-        int front = s_shares.pre[b / per];
-        for (int i = b / per * per; i < b; ++i) front += visit(c, i).n;
-        const long long u = (long long)front * pairs + (long long)pair * v.n;
+        const long long u = (long long)shares_front(c, s_shares, upto, b) * pairs + (long long)pair * v.n;
         first = shares_owner(u, U, W);
         parts = (int)(shares_owner(u + v.n - 1, U, W) - first) + 1;
     }
@@ -276,30 +308,56 @@ k_cache_join(CacheArgs c, int row_tile, int workgroups) {
     if (lane == 0) s_red[wv] = mx;
     __syncthreads();
     mx = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    for (int p = tid; p < parts; p += 256) s_w[p] = s_w[p] == NEG_INF ? 0.f : __builtin_amdgcn_exp2f(s_w[p] - mx);
-    __syncthreads();
 
-    // wave wv takes the parts wv, wv + 4, ..; a lane the channels lane, lane + 64, ..
-    float den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int p = wv; p < parts; p += 4) {
-        const float wp = s_w[p];
-        if (wp == 0.f) continue;                         // (whatever it holds)
-        den += wp;
+    // a lane has the channels 2 lane, 2 lane + 1, and the two 128 behind them
+    const int ch = 2 * lane;
+    float den = 0.f;
+    float2 o[2] = {{0.f, 0.f}, {0.f, 0.f}};
+    auto take = [&](int p0, auto n) {
+        constexpr int N = decltype(n)::value;
+        float2 x[N][2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (64 * k + lane < c.d) o[k] = fmaf(wp, O[(long long)p * row_tile * c.d + 64 * k + lane], o[k]);
+        for (int i = 0; i < N; ++i) {
+            const float* at = O + (long long)min(p0 + 4 * i, parts - 1) * row_tile * c.d;
+            x[i][0] = *reinterpret_cast<const float2*>(at + (ch < c.d ? ch : 0));
+            if (c.d > 128) x[i][1] = *reinterpret_cast<const float2*>(at + (128 + ch < c.d ? 128 + ch : 0));
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float l = p0 + 4 * i < parts ? s_w[p0 + 4 * i] : NEG_INF;
+            if (l == NEG_INF) continue;                  // (whatever it holds)
+            const float wp = __builtin_amdgcn_exp2f(l - mx);
+            den += wp;
+            o[0].x = fmaf(wp, x[i][0].x, o[0].x);
+            o[0].y = fmaf(wp, x[i][0].y, o[0].y);
+            if (c.d > 128) {
+                o[1].x = fmaf(wp, x[i][1].x, o[1].x);
+                o[1].y = fmaf(wp, x[i][1].y, o[1].y);
+            }
+        }
+    };
+    int p0 = wv;
+    for (; p0 + 16 < parts; p0 += 32) take(p0, std::integral_constant<int, 8>{});
+    if (p0 + 4 < parts) { take(p0, std::integral_constant<int, 4>{}); p0 += 16; }
+    if (p0 < parts) take(p0, std::integral_constant<int, 1>{});
+    if (lane == 0) s_den[wv] = den;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        s_o[wv][128 * k + ch] = o[k].x;
+        s_o[wv][128 * k + ch + 1] = o[k].y;
     }
-    if (lane == 0) s_red[wv] = den;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s_o[wv][64 * k + lane] = o[k];
     __syncthreads();
-    den = s_red[0] + s_red[1] + s_red[2] + s_red[3];
+    den = (s_den[0] + s_den[1]) + (s_den[2] + s_den[3]);
     const float inv = den > 0.f ? 1.0f / den : 0.f;
     const int hl = r / c.T, tk = r - hl * c.T, h = kv * c.G + hl;
-    if (tid < c.d) {
-        const float sum = (s_o[0][tid] + s_o[1][tid]) + (s_o[2][tid] + s_o[3][tid]);
-        T* out = reinterpret_cast<T*>(c.O) + b * c.qsb + h * c.qsh + tk * c.qsl;
-        Elem<T>::store1(out + tid, sum * inv);
+    if (4 * tid < c.d) {
+        f32x4 sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 4 * tid + e;
+            sum[e] = ((s_o[0][i] + s_o[1][i]) + (s_o[2][i] + s_o[3][i])) * inv;
+        }
+        store4(reinterpret_cast<T*>(c.O) + b * c.qsb + h * c.qsh + tk * c.qsl + 4 * tid, sum);
     }
     if (tid == 0) {
         const float l2 = mx + log2f(den);
@@ -308,39 +366,53 @@ k_cache_join(CacheArgs c, int row_tile, int workgroups) {
     }
 }
 
-// weight[page][kv][slot] += sum over the KV head's rows of 2^(score - lse), a thread to a position.
+// weight[page][kv][slot] += sum over the KV head's rows of 2^(score - lse): a thread to four positions (of one page), eight
+// blocks of a (sequence, KV head) to a trip, trips dealt out evenly.
 __global__ void __launch_bounds__(256)
 k_cache_weights(CacheArgs c, int row_tile) {
     __shared__ Shares<256> s_shares;
     const int R = c.G * c.T, rows = min(R, row_tile);
-    const int total = shares_scan(c, s_shares);
-    // two blocks of (sequence, KV head) to a trip; trips are dealt out evenly
+    int upto, base;
+    const int total = shares_scan(c, s_shares, upto);
     const long long items = (long long)total * c.Hkv;
     long long i = items * blockIdx.x / gridDim.x;
     const long long end = items * (blockIdx.x + 1) / gridDim.x;
     if (i >= end) return;
-    int base;
     Visit v;
-    int b = shares_find(c, s_shares, (int)(i / c.Hkv), &base, &v);
+    int b = shares_find(c, s_shares, upto, (int)(i / c.Hkv), &base, &v);
     int kv = (int)((i - (long long)base * c.Hkv) / v.n), blk = (int)(i - (long long)base * c.Hkv - (long long)kv * v.n);
-    const int half = threadIdx.x >> 7, k = threadIdx.x & 127;
+    const int eighth = threadIdx.x >> 5, k = 4 * (threadIdx.x & 31);
     while (i < end) {
         const int n = (int)min((long long)(v.n - blk), end - i);
-        for (int j = half; j < n; j += 2) {
+        for (int j = eighth; j < n; j += 8) {
             const int pos = v.block(blk + j) * kUnit + k;
             if (pos >= v.len) continue;
             const int e = c.table[(long long)b * c.width + pos / c.page];
             if ((unsigned)e >= (unsigned)c.num_pages) continue;
-            float sum = 0.f;
+            float* out = c.weight + ((long long)e * c.Hkv + kv) * c.page + pos % c.page;
+            const f32x4 old = *reinterpret_cast<const f32x4*>(out);
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
             for (int rt = 0; rt < c.row_tiles; ++rt) {
-                const long long u = (long long)base * c.Hkv * c.row_tiles + (long long)(kv * c.row_tiles + rt) * v.n + blk + j;
+                const int pair = kv * c.row_tiles + rt;
+                const long long u = c.whole ? ((long long)b * c.Hkv * c.row_tiles + pair) * c.whole + blk + j
+                                            : (long long)base * c.Hkv * c.row_tiles + (long long)pair * v.n + blk + j;
                 const float* s = c.scores + u * rows * kUnit + k;
                 const float* l = c.row_lse + ((long long)b * c.Hkv + kv) * R + rt * row_tile;
                 const int here = min(rows, R - rt * row_tile);
-                for (int q = 0; q < here; ++q) sum += __builtin_amdgcn_exp2f(fmaf(s[q * kUnit], c.scale_log2, -l[q]));
+#pragma unroll 4
+                for (int q = 0; q < here; ++q) {
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(s + q * kUnit);
+                    const float l2 = l[q];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) sum[t] += __builtin_amdgcn_exp2f(fmaf(x[t], c.scale_log2, -l2));
+                }
             }
-            float* out = c.weight + ((long long)e * c.Hkv + kv) * c.page + pos % c.page;
-            *out += sum;
+            // (slots behind the end belong to nobody yet: they keep what they hold)
+            if (pos + 3 < v.len) {
+                *reinterpret_cast<f32x4*>(out) = old + sum;
+            } else {
+                for (int t = 0; pos + t < v.len; ++t) out[t] = old[t] + sum[t];
+            }
         }
         i += n;
         blk += n;
@@ -372,7 +444,9 @@ bool cache_attn_plan(const CacheArgs& c, int dtype, bool accumulate, CachePlan* 
     const long long U = c.batch * blocks * pairs;
     const long long W = std::min<long long>(kCacheWorkgroups, (U + kLeastUnits - 1) / kLeastUnits);
     p->workgroups = (int)std::max(1ll, W);
-    const long long slots = p->workgroups + c.batch * pairs;
+    p->whole = blocks <= kWholeBlocks ? (int)blocks : 0;
+    if (p->whole) p->workgroups = (int)(c.batch * pairs);
+    const long long slots = p->whole ? 0 : p->workgroups + c.batch * pairs;
     p->part_rows = (size_t)slots * p->row_tile;
     p->part_bytes = (p->part_rows * (c.d + 1) * sizeof(float) + 255) / 256 * 256;
     p->score_bytes = accumulate ? (size_t)U * (size_t)std::min<long long>(R, p->row_tile) * kUnit * sizeof(float) : 0;
@@ -408,13 +482,15 @@ hipError_t launch_cache_attn(const CacheArgs& c, int dtype, const CachePlan& pla
         default: break;
     }
     if (e != hipSuccess) return e;
-    const dim3 rows((unsigned)(c.batch * c.Hkv * c.G * c.T));
-    if (dtype == RR_BF16) hipLaunchKernelGGL(k_cache_join<bf16_t>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
-    else hipLaunchKernelGGL(k_cache_join<float>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
-    e = hipGetLastError();
+    if (!plan.whole) {
+        const dim3 rows((unsigned)(c.batch * c.Hkv * c.G * c.T));
+        if (dtype == RR_BF16) hipLaunchKernelGGL(k_cache_join<bf16_t>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
+        else hipLaunchKernelGGL(k_cache_join<float>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess || !c.scores) return e;
     const long long items = c.batch * most_blocks(c.L, c.T, c.window, c.sinks) * c.Hkv;
-    hipLaunchKernelGGL(k_cache_weights, dim3((unsigned)std::min(1024ll, (items + 1) / 2)), dim3(256), 0, st, c, plan.row_tile);
+    hipLaunchKernelGGL(k_cache_weights, dim3((unsigned)std::min(2048ll, (items + 7) / 8)), dim3(256), 0, st, c, plan.row_tile);
     return hipGetLastError();
 }
 

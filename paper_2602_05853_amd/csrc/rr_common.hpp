@@ -223,13 +223,14 @@ struct CacheArgs {
     float scale_log2;           // log2(e) / sqrt(d)
     // of a launch
     int row_tiles;              // a KV head's G T rows, so many at a time
+    int whole;                  // 0, or blocks that a sequence visits at most: a workgroup takes all of them and there are no parts
     float* part_O; float* part_lse;   // [slot][rows of a tile][d] and [slot][rows of a tile], fp32, log2 units
     float* scores;              // [unit][rows of a tile][128]: products with the keys of 128 positions, -inf where masked; or nullptr
     float* row_lse;             // [batch][Hkv][G T], log2 units, +inf for a row without a key: read by the sums of the weights
 };
 struct CachePlan {
     int row_tile, row_tiles;    // rows to a workgroup, and how many such tiles a KV head has
-    int workgroups;
+    int workgroups, whole;
     size_t part_rows;           // rows of partial results
     size_t part_bytes, score_bytes, row_bytes;
     size_t total() const { return part_bytes + score_bytes + row_bytes; }

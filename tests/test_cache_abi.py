@@ -49,6 +49,7 @@ def test_paged_attention_refusals():
     assert attn(Q=None) == bd.RR_ERR_NULL and attn(O=None) == bd.RR_ERR_NULL
     for name in ("K", "V", "table", "length"):
         assert attn(c=pages(**{name: None})) == bd.RR_ERR_NULL
+    assert attn(c=pages(weight=FAKE + 4), flags=1) == bd.RR_ERR_SHAPE
     assert attn(c=pages(weight=None), flags=1) == bd.RR_ERR_NULL and attn(c=pages(weight=None), ws=None) == bd.RR_ERR_WORKSPACE
     assert bd.lib.rr_paged_attn(C.byref(shape()), FAKE, None, 0, 0, 0, FAKE, None, FAKE * 16, 1 << 40, None) == bd.RR_ERR_NULL
     assert bd.lib.rr_paged_attn(None, FAKE, C.byref(pages()), 0, 0, 0, FAKE, None, FAKE * 16, 1 << 40, None) == bd.RR_ERR_NULL
@@ -111,11 +112,11 @@ def test_window_refusals():
     for B in (0, 8, 24, 144, -16):
         assert call(s=shape(Lq=4096), sf=FAKE, B=B) == bd.RR_ERR_SHAPE
     # a workspace counts where the call takes one
-    assert call(ws=FAKE * 16, n=16) == bd.RR_ERR_WORKSPACE and call(ws=FAKE * 16 + 8, n=1 << 40) == bd.RR_ERR_WORKSPACE
+    assert call(window=1000, ws=FAKE * 16, n=16) == bd.RR_ERR_WORKSPACE and call(window=1000, ws=FAKE * 16 + 8, n=1 << 40) == bd.RR_ERR_WORKSPACE
 
     def room(s, window=100):
         return bd.lib.rr_window_workspace_bytes(C.byref(s), window, 0)
-    assert room(shape()) > 0 and room(shape(Lq=8)) > 0 and room(shape(Lq=9)) == 0 and room(shape(Lq=17, Hq=8)) == 0
+    assert room(shape(), 1000) > 0 and room(shape(Lq=8), 1000) > 0 and room(shape()) == 0 and room(shape(Lq=9)) == 0 and room(shape(Lq=17, Hq=8)) == 0
     assert room(shape(), 0) == 0 and room(shape(d=9)) == 0
 
 
