@@ -332,7 +332,7 @@ int rr_dense_attn_ws(const rr_shape* shape, const void* Q, const void* K, const 
  *              most 16 positions and 32 query rows per KV head then share the keys of a KV head out among several workgroups
  *              and read them once for all its query heads.  rr_window_workspace_bytes() is 0 for every other call, and for such
  *              steps that see few keys, which run that way without one.
- * Any L, d and strides of the conventions above.  bf16 with d = 128 (packed: B = 128) runs on a kernel of its own, which rounds
+ * Any L up to 2^30 (so have the caches below and rr_key_weights), d and strides of the conventions above.  bf16 with d = 128 (packed: B = 128) runs on a kernel of its own, which rounds
  * the probabilities to bf16; such steps and all other shapes hold nothing in fewer than 32 bits.  An infinite
  * or NaN value of V that no query of a launch's tile sees does not reach it; one that a query in the same tile sees makes the
  * channel NaN in that tile's other rows, as zero times infinity does.
@@ -426,11 +426,14 @@ int rr_key_weights(const rr_shape* shape, const void* Q, const void* K, const fl
  *              nothing.
  *   to_length  [batch] int32, receives min(n, keep).  May be the cache's own length array.
  *   kept       [batch, Hkv, keep] int32, receives the kept source positions in ascending order, -1 behind them.
+ *   workspace  rr_cache_evict_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards; NULL where that is 0
+ *              (L up to 24576).
  * sinks + recent <= keep (RR_ERR_PARAM).  The q strides, Hq and Lq of the shape are not used (but checked like any other);
  * batch * Hkv <= 65535.  Values move bit for bit.
  */
+size_t rr_cache_evict_workspace_bytes(const rr_shape* shape, const rr_paged_cache* cache);
 int rr_cache_evict(const rr_shape* shape, const rr_paged_cache* cache, int keep, int sinks, int recent, const int32_t* to_table,
-                   int to_width, int32_t* to_length, int32_t* kept, void* hip_stream);
+                   int to_width, int32_t* to_length, int32_t* kept, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Caller-made masks: fills mask->row_count and mask->row_list (and mask->row_order when non-NULL) from

@@ -16,6 +16,7 @@ _NAMES = ("BlockMask", "RRError", "rr_dense_attn", "rr_estimate", "rr_sparse_att
           "rr_workspace_bytes", "rr_attn_workspace_bytes", "rr_estimate_static", "rr_selection_accuracy", "rr_mask_from_dense", "rr_dense_attn_packed", "packed_seq_first",
           "rr_window_attn", "rr_window_workspace_bytes", "PagedCache", "rr_paged_attn", "rr_paged_workspace_bytes", "rr_paged_write",
           "rr_key_weights", "rr_key_weights_workspace_bytes", "rr_cache_evict",
+          "rr_cache_evict_workspace_bytes",
           "RR_FLAG_PROTECT_LAST", "RR_FLAG_DIAGONAL_TOKEN", "LIB_PATH", "OFFSET_MODES")
 
 # (a reload looks them up again)

@@ -34,7 +34,7 @@ EXPORTS = ("rr_version", "rr_status_string", "rr_workspace_bytes", "rr_estimate"
            "rr_mask_from_dense", "rr_dense_attn_packed", "rr_estimate_static", "rr_attn_workspace_bytes",
            "rr_sparse_attn_ws", "rr_dense_attn_ws", "rr_window_workspace_bytes", "rr_window_attn",
            "rr_paged_workspace_bytes", "rr_paged_attn", "rr_paged_write", "rr_key_weights", "rr_cache_evict",
-           "rr_key_weights_workspace_bytes")
+           "rr_key_weights_workspace_bytes", "rr_cache_evict_workspace_bytes")
 
 
 class rr_shape(C.Structure):
@@ -124,7 +124,9 @@ def _load() -> C.CDLL:
     lib.rr_key_weights_workspace_bytes.argtypes = [C.POINTER(rr_shape)]
     lib.rr_cache_evict.restype = C.c_int
     lib.rr_cache_evict.argtypes = [C.POINTER(rr_shape), C.POINTER(rr_paged_cache), C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int,
-                                   C.c_void_p, C.c_void_p, C.c_void_p]
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.rr_cache_evict_workspace_bytes.restype = C.c_size_t
+    lib.rr_cache_evict_workspace_bytes.argtypes = [C.POINTER(rr_shape), C.POINTER(rr_paged_cache)]
     return lib
 
 
@@ -658,17 +660,26 @@ def rr_key_weights(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, out: Opt
     return out
 
 
-def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int = 0, recent: int = 0,
-                   length: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
-                   stream: Optional[torch.cuda.Stream] = None):
-    """Holds every sequence to `keep` positions by accumulated weight, head by head, into the pages of `table` [batch, width]
-    (of the same pools, none of them in use).  Returns the cache over those pages and the kept source positions [batch, Hkv,
-    keep] (-1 behind the last)."""
-    c = cache.c_struct()
+def rr_cache_evict_workspace_bytes(cache: PagedCache) -> int:
+    return lib.rr_cache_evict_workspace_bytes(C.byref(_pool_shape(cache)), C.byref(cache.c_struct()))
+
+
+def _pool_shape(cache: PagedCache) -> rr_shape:
+    """(no rows of queries belong to the call: the pool's own layout in their place)"""
     K = cache.K
     (batch, width), (_, Hkv, page, d), k = cache.table.shape, K.shape, K.stride()
-    # (no rows of queries belong to the call: the pool's own layout in their place)
-    shp = rr_shape(batch, width * page, Hkv, Hkv, d, _dtype_code(K), k[0], k[1], k[2], k[0], k[1], k[2], 1)
+    return rr_shape(batch, width * page, Hkv, Hkv, d, _dtype_code(K), k[0], k[1], k[2], k[0], k[1], k[2], 1)
+
+
+def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int = 0, recent: int = 0,
+                   length: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Holds every sequence to `keep` positions by accumulated weight, head by head, into the pages of `table` [batch, width]
+    (of the same pools, none of them in use).  Returns the cache over those pages and the kept source positions [batch, Hkv,
+    keep] (-1 behind the last).  Without `workspace` one is allocated where it is needed."""
+    c = cache.c_struct()
+    K, shp = cache.K, _pool_shape(cache)
+    batch, Hkv = shp.batch, shp.Hkv
     if keep < 1:
         raise RRError(RR_ERR_PARAM)
     if table.dim() != 2:
@@ -683,7 +694,10 @@ def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int
     else:
         _check_array(kept, torch.int32, (batch, Hkv, keep))
     index = K.get_device()
-    _on_device(index, table, length, kept)
+    _on_device(index, table, length, kept, workspace)
+    if workspace is None:
+        n = lib.rr_cache_evict_workspace_bytes(C.byref(shp), C.byref(c))
+        workspace = torch.empty(n, dtype=torch.uint8, device=K.device) if n else None
     _call(index, stream, lib.rr_cache_evict, C.byref(shp), C.byref(c), keep, sinks, recent, table.data_ptr(), table.shape[1],
-          length.data_ptr(), kept.data_ptr())
+          length.data_ptr(), kept.data_ptr(), _ptr(workspace), _bytes(workspace))
     return PagedCache(cache.K, cache.V, table, length, cache.weight), kept

@@ -1,6 +1,7 @@
 // C ABI of window attention, of the paged cache and of key weights (see include/rr_attn.h): argument checks on the host, then
 // launches.
 #include "rr_common.hpp"
+#include "rr_cache.hpp"
 #include "rr_check.hpp"
 
 #include <algorithm>
@@ -9,7 +10,7 @@ namespace {
 
 using namespace rr;
 
-constexpr int kMostPositions = 0x7fffff00;      // a block behind the last one still has a 32-bit position
+constexpr int kMostPositions = 1 << 30;         // blocks and strides behind the last position still have 32-bit positions
 
 // The layout that outputs are written in gives every element a place of its own
 bool outputs_distinct(const rr_shape* s, int rows) {
@@ -68,7 +69,8 @@ int check_cache(const rr_shape* shape, const rr_paged_cache* cache, CacheArgs* c
     c->psb = g.ksb; c->ksh = g.ksh; c->ksl = g.ksl;
     c->K = cache->K; c->V = cache->V; c->weight = cache->weight;
     c->table = cache->table; c->length = cache->length;
-    c->page = cache->page; c->num_pages = cache->num_pages; c->width = cache->width;
+    set_page(c, cache->page);
+    c->num_pages = cache->num_pages; c->width = cache->width;
     c->scale_log2 = (float)(1.4426950408889634 / sqrt((double)g.d));
     return RR_OK;
 }
@@ -178,8 +180,13 @@ RR_API int rr_paged_write(const rr_shape* shape, const rr_paged_cache* cache, co
     return launch_cache_write(c, shape->dtype, a, cache->K, cache->V, (hipStream_t)hip_stream) == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
 }
 
+RR_API size_t rr_cache_evict_workspace_bytes(const rr_shape* shape, const rr_paged_cache* cache) {
+    CacheArgs c;
+    return check_cache(shape, cache, &c, true) == RR_OK && (long long)c.batch * c.Hkv <= 65535 ? cache_evict_bytes(c) : 0;
+}
+
 RR_API int rr_cache_evict(const rr_shape* shape, const rr_paged_cache* cache, int keep, int sinks, int recent, const int32_t* to_table,
-                          int to_width, int32_t* to_length, int32_t* kept, void* hip_stream) {
+                          int to_width, int32_t* to_length, int32_t* kept, void* workspace, size_t workspace_bytes, void* hip_stream) {
     CacheArgs c;
     const int rc = check_cache(shape, cache, &c);
     if (rc != RR_OK) return rc;
@@ -188,8 +195,10 @@ RR_API int rr_cache_evict(const rr_shape* shape, const rr_paged_cache* cache, in
     // a target holds what is kept of the longest sequence
     if (to_width < 1 || (long long)to_width * c.page < std::min(keep, c.L)) return RR_ERR_SHAPE;
     if (!aligned16(cache->weight) || (long long)c.batch * c.Hkv > 65535) return RR_ERR_SHAPE;
+    const size_t need = cache_evict_bytes(c);
+    if (need && (!workspace || workspace_bytes < need || misaligned256(workspace))) return RR_ERR_WORKSPACE;
     const CacheEvictArgs a = {keep, sinks, recent, to_table, to_width, to_length, kept};
-    return launch_cache_evict(c, shape->dtype, a, cache->K, cache->V, (hipStream_t)hip_stream) == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
+    return launch_cache_evict(c, shape->dtype, a, cache->K, cache->V, workspace, (hipStream_t)hip_stream) == hipSuccess ? RR_OK : RR_ERR_LAUNCH;
 }
 
 RR_API size_t rr_key_weights_workspace_bytes(const rr_shape* shape) {

@@ -8,13 +8,31 @@ namespace rr {
 namespace {
 
 constexpr int kUnit = 128;                      // keys of a block
-constexpr int kLeastUnits = 2;                  // blocks a workgroup takes at least, where there are as many
+#ifndef RR_LU
+#define RR_LU 2
+#endif
+constexpr int kLeastUnits = RR_LU;                  // blocks a workgroup takes at least, where there are as many
 
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef const __attribute__((address_space(4))) int32_t* scalar_words_t;   // read with scalar loads
 #else
 typedef const int32_t* scalar_words_t;                                     // the host pass only parses the kernels
 #endif
+
+// position / page.  Pages are multiples of 16, so n = position / 16 < 2^27 is divided by p = page / 16: with l the bits of p - 1,
+// s = 27 + l and M = ceil(2^s / p) <= 2^28, M p - 2^s < p <= 2^l, so n (M p - 2^s) < 2^s and n M / 2^s has the quotient as its
+// whole part.  (A 32-bit division is some forty vector instructions: they were half of a sweep over a long cache's weights.)
+inline void set_page(CacheArgs* c, int page) {
+    c->page = page;
+    const unsigned p = (unsigned)page >> 4;
+    int l = 0;
+    while ((1u << l) < p) ++l;
+    c->page_shift = 27 + l;
+    c->page_mul = (unsigned)(((1ull << c->page_shift) + p - 1) / p);
+}
+__host__ __device__ inline int page_of(const CacheArgs& c, int pos) {
+    return (int)(((unsigned long long)((unsigned)pos >> 4) * c.page_mul) >> c.page_shift);
+}
 
 // The blocks that a step at the end of `len` positions visits: 0 .. ns - 1, which hold sinks, then those from first_w to the end.
 struct Visit {

@@ -13,6 +13,9 @@
 //
 // Weights: the first kernel also keeps its scores (4 bytes per row and key against the 4 d and 8 d of a key's K and V), and a
 // third adds exp(score - lse) over the rows of a KV head, in the order of the rows, to the positions' sums.
+#ifndef RR_WB
+#define RR_WB 4
+#endif
 #include "rr_cache.hpp"
 #include "rr_attn_frag.hpp"
 
@@ -24,7 +27,7 @@ namespace rr {
 namespace {
 
 constexpr int kCacheWorkgroups = 512;                   // two per compute unit, all resident
-constexpr int kWholeBlocks = 4;                         // sequences that visit at most so many are not shared out
+constexpr int kWholeBlocks = RR_WB;                         // sequences that visit at most so many are not shared out
 
 __device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16_t* p, const f32x4& v) {
@@ -106,7 +109,7 @@ k_cache_attn(CacheArgs c) {
 #pragma unroll
             for (int tl = 0; tl < TL; ++tl) {
                 const int key = first_key(st, tl);
-                entry[tl] = c.table ? ((scalar_words_t)c.table)[(long long)b * c.width + min(key, q_last) / c.page] : 0;
+                entry[tl] = c.table ? ((scalar_words_t)c.table)[(long long)b * c.width + page_of(c, min(key, q_last))] : 0;
             }
         };
         F kf[TL];
@@ -118,7 +121,7 @@ k_cache_attn(CacheArgs c) {
                 key0[tl] = first_key(st, tl);
                 const bool in = key0[tl] < v.len && (!c.table || (unsigned)entry[tl] < (unsigned)c.num_pages);
                 last[tl] = in ? min(15, v.len - 1 - key0[tl]) : -1;
-                at[tl] = c.table ? (long long)entry[tl] * c.psb + (long long)(key0[tl] % c.page) * c.ksl
+                at[tl] = c.table ? (long long)entry[tl] * c.psb + (long long)(key0[tl] - page_of(c, key0[tl]) * c.page) * c.ksl
                                  : (long long)b * c.psb + (long long)key0[tl] * c.ksl;
                 if (last[tl] == 15) kf[tl].load(K + at[tl] + k_off, d, gq);
                 else if (in) kf[tl].load(K + at[tl] + (long long)min(x, last[tl]) * c.ksl, d, gq);
@@ -387,9 +390,9 @@ k_cache_weights(CacheArgs c, int row_tile) {
         for (int j = eighth; j < n; j += 8) {
             const int pos = v.block(blk + j) * kUnit + k;
             if (pos >= v.len) continue;
-            const int e = c.table[(long long)b * c.width + pos / c.page];
+            const int pg = page_of(c, pos), e = c.table[(long long)b * c.width + pg];
             if ((unsigned)e >= (unsigned)c.num_pages) continue;
-            float* out = c.weight + ((long long)e * c.Hkv + kv) * c.page + pos % c.page;
+            float* out = c.weight + ((long long)e * c.Hkv + kv) * c.page + (pos - pg * c.page);
             const f32x4 old = *reinterpret_cast<const f32x4*>(out);
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
             for (int rt = 0; rt < c.row_tiles; ++rt) {

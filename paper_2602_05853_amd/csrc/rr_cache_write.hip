@@ -23,7 +23,7 @@ k_cache_write(CacheArgs c, CacheWriteArgs a, u32x4* K, u32x4* V, int chunks, int
         if (t >= count) return;                                        // (t only grows)
         const int pos = len - count + t;
         if (pos < 0) continue;
-        const int e = c.table[(long long)b * c.width + pos / c.page], slot = pos % c.page;
+        const int pg = page_of(c, pos), e = c.table[(long long)b * c.width + pg], slot = pos - pg * c.page;
         if ((unsigned)e >= (unsigned)c.num_pages) continue;
         const long long from = ((b * c.qsb + kv * c.qsh + t * c.qsl) >> log_piece) + ch;
         const long long to = ((e * c.psb + kv * c.ksh + slot * c.ksl) >> log_piece) + ch;

@@ -219,6 +219,8 @@ struct CacheArgs {
     const int32_t* table;       // [batch][width]
     const int32_t* length;      // [batch]
     int page, num_pages, width;
+    unsigned page_mul;          // position / page without a division, see page_of
+    int page_shift;
     int window, sinks;          // as above; window = L + T: the whole context
     float scale_log2;           // log2(e) / sqrt(d)
     // of a launch
@@ -252,7 +254,8 @@ struct CacheEvictArgs {
     int32_t* to_length;
     int32_t* kept;              // [batch][Hkv][keep]
 };
-hipError_t launch_cache_evict(const CacheArgs& c, int dtype, const CacheEvictArgs& a, void* K, void* V, hipStream_t st);
+size_t cache_evict_bytes(const CacheArgs& c);              // 0: without a workspace
+hipError_t launch_cache_evict(const CacheArgs& c, int dtype, const CacheEvictArgs& a, void* K, void* V, void* workspace, hipStream_t st);
 
 // (9) softmax weights that every key gets from the queries of a call: out[b][kv][key], fp32.
 size_t key_weights_bytes(const Geom& g, int dtype);         // 0: without a workspace

@@ -6,6 +6,9 @@
 // each with an online softmax of its own, joined in LDS at the end.  The keys are two runs of 16-key tiles, the sinks' and the
 // window's; only tiles at a border (of the window, the sinks, the sequence, causality) are masked key by key.
 // Arithmetic: nothing is held in fewer than 32 bits (rr_attn_frag.hpp).
+#ifndef RR_QW
+#define RR_QW (32*512)
+#endif
 #include "rr_attn_frag.hpp"
 
 #include <algorithm>
@@ -226,7 +229,7 @@ hipError_t launch_window_generic(const Geom& g, int dtype, const WindowArgs& a, 
                     if (rows >= 64 * 512) return launch(k_window_generic<bf16_t, N, D, 4, 2, 4, 2>, 64, 4);
                 return launch(k_window_generic<bf16_t, N, D, 2, 2, 4, 2>, 32, 4);
             }
-            if (rows >= 32 * 512) return launch(k_window_generic<float, N, D, 2, 1, 8, 2>, 32, 8);
+            if (rows >= RR_QW) return launch(k_window_generic<float, N, D, 2, 1, 8, 2>, 32, 8);
             return launch(k_window_generic<float, N, D, 1, 1, 8, 2>, 16, 8);
         }
     };

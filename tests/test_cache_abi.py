@@ -67,11 +67,11 @@ def test_paged_attention_refusals():
     s = shape()
     s.kv_stride_l = 130
     assert attn(s=s) == bd.RR_ERR_SHAPE
-    s = shape(L=0x7fffffff)
+    s = shape(L=(1 << 30) + 1)
     assert attn(s=s, c=pages(page=1 << 20, width=1 << 20)) == bd.RR_ERR_SHAPE
     # more blocks than a launch's 32-bit sums hold
-    s = shape(L=0x7fffff00, batch=200)
-    assert attn(s=s, c=pages(page=1 << 20, width=1 << 12)) == bd.RR_ERR_SHAPE
+    s = shape(L=1 << 30, batch=300)
+    assert attn(s=s, c=pages(page=1 << 20, width=1 << 10)) == bd.RR_ERR_SHAPE
 
 
 def workspace(s, c=None, window=0, sinks=0, flags=0):
@@ -127,8 +127,15 @@ def test_write_weights_and_evict_refusals():
     assert write(c=pages(weight=None), weight=FAKE) == bd.RR_ERR_NULL
     assert write(K=FAKE + 2) == bd.RR_ERR_SHAPE and write(s=shape(batch=70000)) == bd.RR_ERR_SHAPE
 
-    def evict(s=None, c=None, keep=100, sinks=4, recent=10, to=FAKE, width=2, length=FAKE, kept=FAKE):
-        return bd.lib.rr_cache_evict(C.byref(s or shape()), C.byref(c or pages()), keep, sinks, recent, to, width, length, kept, None)
+    def evict(s=None, c=None, keep=100, sinks=4, recent=10, to=FAKE, width=2, length=FAKE, kept=FAKE, ws=None, n=0):
+        return bd.lib.rr_cache_evict(C.byref(s or shape()), C.byref(c or pages()), keep, sinks, recent, to, width, length, kept, ws, n, None)
+    long, wide = shape(L=30000), pages(width=500)
+    assert bd.lib.rr_cache_evict_workspace_bytes(C.byref(shape()), C.byref(pages())) == 0
+    need = bd.lib.rr_cache_evict_workspace_bytes(C.byref(long), C.byref(wide))
+    assert need >= 3 * 16 * 2048 * 4
+    for ws, n in ((None, 1 << 40), (FAKE * 16, need - 1), (FAKE * 16 + 64, 1 << 40)):
+        assert evict(s=long, c=wide, ws=ws, n=n) == bd.RR_ERR_WORKSPACE
+    assert evict(c=pages(weight=FAKE + 4)) == bd.RR_ERR_SHAPE
     assert evict(c=pages(weight=None)) == bd.RR_ERR_NULL and evict(to=None) == bd.RR_ERR_NULL and evict(length=None) == bd.RR_ERR_NULL
     assert evict(kept=None) == bd.RR_ERR_NULL
     assert evict(keep=0) == bd.RR_ERR_PARAM and evict(sinks=-1) == bd.RR_ERR_PARAM and evict(recent=-1) == bd.RR_ERR_PARAM

@@ -105,13 +105,13 @@ def evict_reference(cache, keep, sinks, recent):
         n = min(max(n, 0), cache.table.shape[1] * cache.K.shape[2])
         for kv in range(cache.K.shape[1]):
             w, good = positions(cache, b, n, kv, "weight")
-            w = w.tolist()
+            w, good = w.tolist(), good.tolist()
             if n <= keep:
                 out.append(list(range(n)))
                 continue
             def rank(j):
                 value = math.inf if math.isnan(w[j]) else w[j]
-                return (not bool(good[j]), not math.isnan(w[j]), -value, j)
+                return (not good[j], not math.isnan(w[j]), -value, j)
             middle = sorted(range(sinks, n - recent), key=rank)[:keep - sinks - recent]
             out.append(sorted(list(range(sinks)) + middle + list(range(n - recent, n))))
     return out
@@ -134,13 +134,13 @@ def evict(cache, keep, sinks, recent):
         assert int(new.length[i]) == min(n, keep)
         for kv in range(Hkv):
             w = want[i * Hkv + kv]
-            got = kept[i, kv].tolist()
-            assert got == w + [-1] * (keep - len(w)), (i, kv)
-            for r, pos in enumerate(w):
-                s, t = int(grown.table[i, pos // page]), int(fresh[i, r // page])
-                if 0 <= s < grown.K.shape[0]:
-                    for x in before:
-                        x[t, kv, r % page] = x[s, kv, pos % page]
+            assert kept[i, kv].tolist() == w + [-1] * (keep - len(w)), (i, kv)
+            pos, r = torch.tensor(w, dtype=torch.int64, device=DEV), torch.arange(len(w), device=DEV)
+            s, t = grown.table[i].long()[pos // page], fresh[i].long().to(DEV)[r // page]
+            good = (s >= 0) & (s < grown.K.shape[0])
+            pos, r, s, t = pos[good], r[good], s[good], t[good]
+            for x in before:
+                x[t, kv, r % page] = x[s, kv, pos % page]
     for got, w in zip((grown.K, grown.V, grown.weight), before):
         assert torch.equal(got.view(torch.int32 if got.dtype == torch.float32 else torch.int16),
                            w.view(torch.int32 if w.dtype == torch.float32 else torch.int16))
@@ -173,6 +173,17 @@ def test_evict_equal_and_special_weights():
 @pytest.mark.parametrize("n,keep", [(5000, 2500), (1024, 1023), (1025, 1024), (2048, 7), (40000, 20000)])
 def test_evict_longer(n, keep):
     evict(make([n], 1, 8, 64, weight=True), keep, min(4, keep), keep // 4)
+
+
+@pytest.mark.parametrize("keep,sinks,recent", [(20000, 4, 3000), (24999, 0, 0), (5, 2, 3), (1, 0, 0), (8192, 8000, 192), (30000, 5, 9)])
+def test_evict_caches_of_more_positions_than_lds_holds(keep, sinks, recent):
+    """Sequences of several chunks of 8192 next to short ones, equal weights across chunk borders, a page that is none."""
+    cache = make([25000, 8192, 300, 0, 40961], 2, 8, 48, weight=True)
+    w = cache.weight
+    w[cache.table[4, :].clamp(min=0).long()] = torch.randint(0, 3, (cache.table.shape[1], 2, 48), device=DEV).float()
+    w[cache.table[0, 3].long()] = math.nan
+    cache.table[4, 200] = -1
+    evict(cache, keep, sinks, recent)
 
 
 def test_evict_into_its_own_length():
