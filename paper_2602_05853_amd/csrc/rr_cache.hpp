@@ -8,10 +8,6 @@ namespace rr {
 namespace {
 
 constexpr int kUnit = 128;                      // keys of a block
-#ifndef RR_LU
-#define RR_LU 2
-#endif
-constexpr int kLeastUnits = RR_LU;                  // blocks a workgroup takes at least, where there are as many
 
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef const __attribute__((address_space(4))) int32_t* scalar_words_t;   // read with scalar loads
@@ -64,9 +60,9 @@ __device__ __forceinline__ int length_of(const CacheArgs& c, int b) {
 }
 __device__ __forceinline__ Visit visit(const CacheArgs& c, int b) { return visit_of(length_of(c, b), c.T, c.window, c.sinks); }
 
-// The units of a launch, in order: sequence by sequence, `pairs` (KV head and row tile) by pair, block by block.  Workgroup w
-// of W takes units U w / W .. U (w + 1) / W - 1, whatever sequences they belong to, so all end together however uneven the
-// lengths are; the part of a pair that a workgroup computes has slot w + (number of the pair), which is its own: from one
+// The units of a launch, in order: sequence by sequence, `pairs` (KV head and row tile) by pair, block by block.  The W
+// workgroups take U / W or one more of them each, one after the other, whatever sequences they belong to, so all end together
+// however uneven the lengths are; the part of a pair that a workgroup computes has slot w + (number of the pair), which is its own: from one
 // part to the next at least one of the two grows.
 // Every workgroup adds the lengths up for itself: up to 64 sequences a lane each, in every wave (no LDS, no barrier); more, thread t
 // the sequences t per .. t per + per - 1, then a scan over threads.
@@ -147,13 +143,23 @@ __device__ __forceinline__ int shares_front(const CacheArgs& c, const Shares<kTh
     for (int i = b / per * per; i < b; ++i) front += visit(c, i).n;
     return front;
 }
-// Workgroups that take part in U units
-__device__ __forceinline__ long long shares_count(long long U, int workgroups) {
-    const long long most = (U + kLeastUnits - 1) / kLeastUnits;
-    return most < workgroups ? most : workgroups;
-}
-// The workgroup of W that has unit u of U
-__device__ __forceinline__ int shares_owner(long long u, long long U, long long W) { return (int)(((u + 1) * W - 1) / U); }
+// How U units are dealt out to at most `workgroups`: to no more than take them in the same number of units each (fewer parts to
+// join).  All of it in 32 bits: a division of 64 takes over a hundred instructions.
+struct Deal {
+    unsigned W, each, more;                     // the first `more` workgroups have one unit more than `each`
+    __host__ __device__ Deal(unsigned U, unsigned workgroups) {
+        const unsigned most = (U + workgroups - 1) / workgroups;
+        W = most ? (U + most - 1) / most : 0;
+        each = W ? U / W : 0;
+        more = U - each * W;
+    }
+    __device__ __forceinline__ unsigned start(unsigned w) const { return each * w + (w < more ? w : more); }
+    // the workgroup that has unit u
+    __device__ __forceinline__ unsigned owner(unsigned u) const {
+        const unsigned big = more * (each + 1);
+        return u < big ? u / (each + 1) : more + (u - big) / each;
+    }
+};
 
 }  // namespace
 

@@ -13,9 +13,6 @@
 //
 // Weights: the first kernel also keeps its scores (4 bytes per row and key against the 4 d and 8 d of a key's K and V), and a
 // third adds exp(score - lse) over the rows of a KV head, in the order of the rows, to the positions' sums.
-#ifndef RR_WB
-#define RR_WB 4
-#endif
 #include "rr_cache.hpp"
 #include "rr_attn_frag.hpp"
 
@@ -27,7 +24,7 @@ namespace rr {
 namespace {
 
 constexpr int kCacheWorkgroups = 512;                   // two per compute unit, all resident
-constexpr int kWholeBlocks = RR_WB;                         // sequences that visit at most so many are not shared out
+constexpr int kWholeBlocks = 4;                         // sequences that visit at most so many are not shared out
 
 __device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16_t* p, const f32x4& v) {
@@ -55,7 +52,7 @@ k_cache_attn(CacheArgs c) {
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = c.G * c.T, pairs = c.Hkv * c.row_tiles;
 
-    long long u, u_end;
+    unsigned u, u_end;                                  // units (fewer than 2^31)
     Visit v;
     int b, pair, i_lo;
     if (c.whole) {
@@ -65,18 +62,19 @@ k_cache_attn(CacheArgs c) {
         pair = (int)blockIdx.x - b * pairs;
         i_lo = 0;
         v = visit(c, b);
-        u = (long long)blockIdx.x * c.whole;
-        u_end = u + v.n;
+        u = blockIdx.x * (unsigned)c.whole;
+        u_end = u + (unsigned)v.n;
     } else {
         int upto, base;
         const int total = shares_scan(c, s_shares, upto);
-        const long long U = (long long)total * pairs, W = shares_count(U, (int)gridDim.x);
-        if ((long long)blockIdx.x >= W) return;
-        u = U * blockIdx.x / W;
-        u_end = U * (blockIdx.x + 1) / W;
-        b = shares_find(c, s_shares, upto, (int)(u / pairs), &base, &v);
-        pair = (int)((u - (long long)base * pairs) / v.n);
-        i_lo = (int)(u - (long long)base * pairs - (long long)pair * v.n);
+        const Deal deal((unsigned)total * (unsigned)pairs, gridDim.x);
+        if (blockIdx.x >= deal.W) return;
+        u = deal.start(blockIdx.x);
+        u_end = deal.start(blockIdx.x + 1);
+        b = shares_find(c, s_shares, upto, (int)(u / (unsigned)pairs), &base, &v);
+        const unsigned in_b = u - (unsigned)base * (unsigned)pairs;
+        pair = (int)(in_b / (unsigned)v.n);
+        i_lo = (int)(in_b - (unsigned)pair * (unsigned)v.n);
     }
 
     // rows of a tile this lane reads, relative to its first key
@@ -86,8 +84,8 @@ k_cache_attn(CacheArgs c) {
     for (int r = 0; r < 4; ++r) v_off[r] = (long long)(4 * gq + r) * c.ksl;
 
     do {
-        const int blocks = (int)min((long long)(v.n - i_lo), u_end - u);
-        const int kv = pair / c.row_tiles, rt = pair - kv * c.row_tiles;
+        const int blocks = min(v.n - i_lo, (int)(u_end - u));
+        const int kv = c.row_tiles == 1 ? pair : pair / c.row_tiles, rt = pair - kv * c.row_tiles;
         const int q_first = v.len - c.T, q_last = v.len - 1;
 
         // rows that do not exist repeat the last one and are not stored
@@ -95,7 +93,7 @@ k_cache_attn(CacheArgs c) {
         int qpos[QT];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const int rr = min(kQ * rt + 16 * t + x, R - 1), hl = rr / c.T, tk = rr - hl * c.T;
+            const int rr = min(kQ * rt + 16 * t + x, R - 1), hl = c.T == 1 ? rr : rr / c.T, tk = rr - hl * c.T;
             qf[t].load(reinterpret_cast<const T*>(c.Q) + b * c.qsb + (long long)(kv * c.G + hl) * c.qsh + (long long)tk * c.qsl, d, gq);
             qpos[t] = q_first + tk;
         }
@@ -128,6 +126,16 @@ k_cache_attn(CacheArgs c) {
                 else kf[tl] = F{};
             }
         };
+        auto load_values = [&](typename F::V& vf) {      // of the keys loaded last
+#pragma unroll
+            for (int tl = 0; tl < TL; ++tl)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (last[tl] == 15) F::load_v(vf, 4 * tl + r, V + at[tl] + v_off[r], d, x);
+                    else if (last[tl] >= 0) F::load_v(vf, 4 * tl + r, V + at[tl] + (long long)min(4 * gq + r, last[tl]) * c.ksl, d, x);
+                    else F::drop(vf, 4 * tl + r, true);
+                }
+        };
         f32x4 acc[QT][NT];
         float ref[QT], lsum[QT];
         auto walk = [&](auto careful) {
@@ -145,15 +153,7 @@ k_cache_attn(CacheArgs c) {
             }
             for (int st = 0; st < steps; ++st) {
                 typename F::V vf;
-#pragma unroll
-                for (int tl = 0; tl < TL; ++tl) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (last[tl] == 15) F::load_v(vf, 4 * tl + r, V + at[tl] + v_off[r], d, x);
-                        else if (last[tl] >= 0) F::load_v(vf, 4 * tl + r, V + at[tl] + (long long)min(4 * gq + r, last[tl]) * c.ksl, d, x);
-                        else F::drop(vf, 4 * tl + r, true);
-                    }
-                }
+                load_values(vf);
                 f32x4 s[QT][TL];
 #pragma unroll
                 for (int t = 0; t < QT; ++t)
@@ -179,7 +179,7 @@ k_cache_attn(CacheArgs c) {
                     }
                     if (c.scores) {
                         const int rows = min(R, kQ);
-                        float* out = c.scores + (u + st / kSteps) * (long long)rows * kUnit + (st % kSteps) * kStep + 16 * (TL * w + tl) + 4 * gq;
+                        float* out = c.scores + (long long)(u + st / kSteps) * rows * kUnit + (st % kSteps) * kStep + 16 * (TL * w + tl) + 4 * gq;
 #pragma unroll
                         for (int t = 0; t < QT; ++t)
                             if (16 * t + x < rows) *reinterpret_cast<f32x4*>(out + (16 * t + x) * kUnit) = s[t][tl];
@@ -190,7 +190,7 @@ k_cache_attn(CacheArgs c) {
                 auto ahead = [&]() {
                     if (st + 1 < steps) {
                         load_keys(st + 1);
-                        request(min(st + 2, steps - 1));
+                                request(min(st + 2, steps - 1));
                     }
                 };
                 if (!decltype(careful)::value) ahead();
@@ -247,7 +247,7 @@ k_cache_attn(CacheArgs c) {
                 *reinterpret_cast<f32x4*>(c.part_O + (slot * kQ + q) * d + ch) = o;
                 if (ch == 0) c.part_lse[slot * kQ + q] = l > 0.f ? top + log2f(l) : NEG_INF;
             } else {
-                const int rr = kQ * rt + q, hl = rr / c.T, tk = rr - hl * c.T, h = kv * c.G + hl;
+                const int rr = kQ * rt + q, hl = c.T == 1 ? rr : rr / c.T, tk = rr - hl * c.T, h = kv * c.G + hl;
                 store4(reinterpret_cast<T*>(c.O) + b * c.qsb + h * c.qsh + tk * c.qsl + ch, o);
                 if (ch == 0) {
                     const float l2 = top + log2f(l);
@@ -258,7 +258,7 @@ k_cache_attn(CacheArgs c) {
         }
         __syncthreads();                                 // the shares' places are free again
 
-        u += blocks;
+        u += (unsigned)blocks;
         i_lo += blocks;
         if (i_lo == v.n && u < u_end) {
             i_lo = 0;
@@ -288,14 +288,14 @@ k_cache_join(CacheArgs c, int row_tile, int workgroups) {
 
     int upto;
     const int total = shares_scan(c, s_shares, upto);
-    const long long U = (long long)total * pairs, W = shares_count(U, workgroups);
+    const Deal deal((unsigned)total * (unsigned)pairs, (unsigned)workgroups);
     const Visit v = visit(c, b);
     int parts = 0;
     long long first = 0;
     if (v.n > 0) {
-        const long long u = (long long)shares_front(c, s_shares, upto, b) * pairs + (long long)pair * v.n;
-        first = shares_owner(u, U, W);
-        parts = (int)(shares_owner(u + v.n - 1, U, W) - first) + 1;
+        const unsigned u = (unsigned)shares_front(c, s_shares, upto, b) * (unsigned)pairs + (unsigned)pair * (unsigned)v.n;
+        first = deal.owner(u);
+        parts = (int)(deal.owner(u + (unsigned)v.n - 1) - (unsigned)first) + 1;
     }
     const long long slot = first + (long long)b * pairs + pair;
     const float* lse = c.part_lse + slot * row_tile + r % row_tile;
@@ -377,16 +377,17 @@ k_cache_weights(CacheArgs c, int row_tile) {
     const int R = c.G * c.T, rows = min(R, row_tile);
     int upto, base;
     const int total = shares_scan(c, s_shares, upto);
-    const long long items = (long long)total * c.Hkv;
-    long long i = items * blockIdx.x / gridDim.x;
-    const long long end = items * (blockIdx.x + 1) / gridDim.x;
+    const unsigned items = (unsigned)total * (unsigned)c.Hkv, each = (items + gridDim.x - 1) / gridDim.x;
+    unsigned i = min(items, each * blockIdx.x);
+    const unsigned end = min(items, i + each);
     if (i >= end) return;
     Visit v;
-    int b = shares_find(c, s_shares, upto, (int)(i / c.Hkv), &base, &v);
-    int kv = (int)((i - (long long)base * c.Hkv) / v.n), blk = (int)(i - (long long)base * c.Hkv - (long long)kv * v.n);
+    int b = shares_find(c, s_shares, upto, (int)(i / (unsigned)c.Hkv), &base, &v);
+    const unsigned in_b = i - (unsigned)base * (unsigned)c.Hkv;
+    int kv = (int)(in_b / (unsigned)v.n), blk = (int)(in_b - (unsigned)kv * (unsigned)v.n);
     const int eighth = threadIdx.x >> 5, k = 4 * (threadIdx.x & 31);
     while (i < end) {
-        const int n = (int)min((long long)(v.n - blk), end - i);
+        const int n = min(v.n - blk, (int)(end - i));
         for (int j = eighth; j < n; j += 8) {
             const int pos = v.block(blk + j) * kUnit + k;
             if (pos >= v.len) continue;
@@ -417,7 +418,7 @@ k_cache_weights(CacheArgs c, int row_tile) {
                 for (int t = 0; pos + t < v.len; ++t) out[t] = old[t] + sum[t];
             }
         }
-        i += n;
+        i += (unsigned)n;
         blk += n;
         if (blk == v.n && i < end) {
             blk = 0;
@@ -442,11 +443,10 @@ bool cache_attn_plan(const CacheArgs& c, int dtype, bool accumulate, CachePlan* 
     p->row_tile = row_tile_of(c, dtype);
     p->row_tiles = (int)((R + p->row_tile - 1) / p->row_tile);
     const long long pairs = (long long)c.Hkv * p->row_tiles, blocks = most_blocks(c.L, c.T, c.window, c.sinks);
-    // the sums of blocks and the indexes of pairs and rows are 32 bits
-    if ((long long)c.batch * blocks > 0x7fffffff || c.batch * pairs > 0x7fffffff || c.batch * c.Hkv * R > 0x7fffffff) return false;
+    // units, and the indexes of pairs and rows, are 31 bits; a launch is fewer than 2^32 threads
+    if (c.batch * pairs > 0x7fffff || c.batch * c.Hkv * R > 0xffffff || c.batch * pairs * blocks > 0x7fffffff - 4096) return false;
     const long long U = c.batch * blocks * pairs;
-    const long long W = std::min<long long>(kCacheWorkgroups, (U + kLeastUnits - 1) / kLeastUnits);
-    p->workgroups = (int)std::max(1ll, W);
+    p->workgroups = (int)std::max(1ll, std::min<long long>(kCacheWorkgroups, U));
     p->whole = blocks <= kWholeBlocks ? (int)blocks : 0;
     if (p->whole) p->workgroups = (int)(c.batch * pairs);
     const long long slots = p->whole ? 0 : p->workgroups + c.batch * pairs;

@@ -6,9 +6,6 @@
 // each with an online softmax of its own, joined in LDS at the end.  The keys are two runs of 16-key tiles, the sinks' and the
 // window's; only tiles at a border (of the window, the sinks, the sequence, causality) are masked key by key.
 // Arithmetic: nothing is held in fewer than 32 bits (rr_attn_frag.hpp).
-#ifndef RR_QW
-#define RR_QW (32*512)
-#endif
 #include "rr_attn_frag.hpp"
 
 #include <algorithm>
@@ -229,8 +226,10 @@ hipError_t launch_window_generic(const Geom& g, int dtype, const WindowArgs& a, 
                     if (rows >= 64 * 512) return launch(k_window_generic<bf16_t, N, D, 4, 2, 4, 2>, 64, 4);
                 return launch(k_window_generic<bf16_t, N, D, 2, 2, 4, 2>, 32, 4);
             }
-            if (rows >= RR_QW) return launch(k_window_generic<float, N, D, 2, 1, 8, 2>, 32, 8);
-            return launch(k_window_generic<float, N, D, 1, 1, 8, 2>, 16, 8);
+            // (1511 positions, 8 heads of 80, window 200, 95 tiles of 16 queries to a head, us: 16 queries on eight waves 20.0, on four
+            // 18.7, 32 on eight 24.9, on four 21.8: half the reads, but the workgroups no longer fill the chip)
+            if (rows >= 32 * 512) return launch(k_window_generic<float, N, D, 2, 1, 8, 2>, 32, 8);
+            return launch(k_window_generic<float, N, D, 1, 1, 4, 2>, 16, 4);
         }
     };
     using std::integral_constant;
