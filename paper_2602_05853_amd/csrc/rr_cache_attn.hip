@@ -24,7 +24,11 @@ namespace rr {
 namespace {
 
 constexpr int kCacheWorkgroups = 512;                   // two per compute unit, all resident
-constexpr int kWholeBlocks = 4;                         // sequences that visit at most so many are not shared out
+// Sequences that visit few blocks are not shared out: a workgroup to each (and KV head), one launch instead of two.  Shared / not, us,
+// bf16, 32 / 8 heads: 1 sequence of 128 positions 12.1 / 9.6, 512 11.8 / 10.5, 1024 11.9 / 16.3; 16 sequences of 512 14.7 / 11.5, 640
+// 20.0 / 13.8, 1024 20.8 / 19.0, 2048 29.6 / 32.3; 64 of 256 23.9 / 14.7, 1024 51.9 / 42.4, 2048 106 / 95 (but uneven ones of so many
+// blocks would end when the longest does).
+constexpr int kWholeBlocks = 4, kWholeBlocksOfMany = 8, kMany = 128;
 
 __device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16_t* p, const f32x4& v) {
@@ -447,7 +451,7 @@ bool cache_attn_plan(const CacheArgs& c, int dtype, bool accumulate, CachePlan* 
     if (c.batch * pairs > 0x7fffff || c.batch * c.Hkv * R > 0xffffff || c.batch * pairs * blocks > 0x7fffffff - 4096) return false;
     const long long U = c.batch * blocks * pairs;
     p->workgroups = (int)std::max(1ll, std::min<long long>(kCacheWorkgroups, U));
-    p->whole = blocks <= kWholeBlocks ? (int)blocks : 0;
+    p->whole = blocks <= (c.batch * pairs < kMany ? kWholeBlocks : kWholeBlocksOfMany) ? (int)blocks : 0;
     if (p->whole) p->workgroups = (int)(c.batch * pairs);
     const long long slots = p->whole ? 0 : p->workgroups + c.batch * pairs;
     p->part_rows = (size_t)slots * p->row_tile;
