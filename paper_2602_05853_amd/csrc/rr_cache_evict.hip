@@ -196,6 +196,7 @@ constexpr int kChunkThreads = 256, kChunkGroups = 8, kChunk = 4 * kChunkThreads 
 
 struct EvictSpace {
     unsigned* hist;                     // [3][pairs][kBins]: digits of the keys that agree with what the digits before have picked
+    unsigned* pick;                     // [3][pairs][2]: the key's leading digits, and how many of the keys that have them are kept
     int* count;                         // [pairs][chunks][2]: kept for sure (protected or heavier), equal to the last kept weight
     int pairs, chunks;
 };
@@ -206,44 +207,49 @@ k_evict_clear(u32x4* hist, int n) {
     if (i < n) hist[i] = u32x4{0u, 0u, 0u, 0u};
 }
 
-// What the first `digits` digits have picked, by every workgroup for itself from the histograms.
-__device__ __forceinline__ void picked(const EvictSpace& sp, int pair, int want, int digits, int* s_wave, int* s_pick, unsigned* prefix,
-                                       unsigned* mask, int* left) {
+// What the digits up to `digits` - 1 have picked: the last of them from its histogram, by every workgroup for itself, the others as the
+// stage before has left them.
+__device__ __forceinline__ void picked(const EvictSpace& sp, int pair, int want, int digits, bool leave, int* s_wave, int* s_pick,
+                                       unsigned* prefix, unsigned* mask, int* left) {
     constexpr int kPer = kBins / kChunkThreads;
     *prefix = 0u;
-    *mask = 0u;
+    *mask = digits == 0 ? 0u : digits == 1 ? 0xFFE00000u : digits == 2 ? 0xFFFFFC00u : 0xFFFFFFFFu;
     *left = want;
-    for (int digit = 0; digit < digits; ++digit) {
-        const unsigned* hist = sp.hist + ((long long)digit * sp.pairs + pair) * kBins;
-        const int top = kBins - 1 - kPer * (int)threadIdx.x;            // thread t: bins from the top down
-        int h[kPer], sum = 0;
+    if (digits == 0) return;
+    if (digits > 1) {
+        *prefix = sp.pick[((long long)(digits - 2) * sp.pairs + pair) * 2];
+        *left = (int)sp.pick[((long long)(digits - 2) * sp.pairs + pair) * 2 + 1];
+    }
+    const unsigned* hist = sp.hist + ((long long)(digits - 1) * sp.pairs + pair) * kBins;
+    const int top = kBins - 1 - kPer * (int)threadIdx.x;                // thread t: bins from the top down
+    int h[kPer], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) { h[i] = (int)hist[top - i]; sum += h[i]; }
-        int upto = sum;
-        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int i = 0; i < kPer; ++i) { h[i] = (int)hist[top - i]; sum += h[i]; }
+    int upto = sum;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int up = __shfl_up(upto, o);
-            if (lane >= o) upto += up;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(upto, o);
+        if (lane >= o) upto += up;
+    }
+    if (lane == 63) s_wave[w] = upto;
+    __syncthreads();
+    int above = upto - sum;
+#pragma unroll
+    for (int i = 0; i < kChunkThreads / 64; ++i) above += i < w ? s_wave[i] : 0;
+    if (above < *left && *left <= above + sum) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (above < *left && *left <= above + h[i]) { s_pick[0] = top - i; s_pick[1] = *left - above; }
+            above += h[i];
         }
-        __syncthreads();
-        if (lane == 63) s_wave[w] = upto;
-        __syncthreads();
-        int above = upto - sum;
-#pragma unroll
-        for (int i = 0; i < kChunkThreads / 64; ++i) above += i < w ? s_wave[i] : 0;
-        if (above < *left && *left <= above + sum) {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                if (above < *left && *left <= above + h[i]) { s_pick[0] = top - i; s_pick[1] = *left - above; }
-                above += h[i];
-            }
-        }
-        __syncthreads();
-        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
-        *prefix |= (unsigned)s_pick[0] << shift;
-        *mask |= (digit == 2 ? 1023u : 2047u) << shift;
-        *left = s_pick[1];
+    }
+    __syncthreads();
+    *prefix |= (unsigned)s_pick[0] << (digits == 1 ? 21 : digits == 2 ? 10 : 0);
+    *left = s_pick[1];
+    if (leave && threadIdx.x == 0) {
+        sp.pick[((long long)(digits - 1) * sp.pairs + pair) * 2] = *prefix;
+        sp.pick[((long long)(digits - 1) * sp.pairs + pair) * 2 + 1] = (unsigned)*left;
     }
 }
 
@@ -268,7 +274,14 @@ k_evict_chunks(CacheArgs c, CacheEvictArgs a, EvictSpace sp) {
     if (kStage < 3 && want == 0) return;
     unsigned prefix = 0u, mask = 0u;
     int left = 0;
-    if (want > 0) picked(sp, pair, want, kStage < 3 ? kStage : 3, s_scan, s_pick, &prefix, &mask, &left);
+    if (want > 0) {
+        if (kStage < 4) {
+            picked(sp, pair, want, kStage, blockIdx.x == 0, s_scan, s_pick, &prefix, &mask, &left);
+        } else {
+            prefix = sp.pick[(2ll * sp.pairs + pair) * 2];
+            left = (int)sp.pick[(2ll * sp.pairs + pair) * 2 + 1];
+        }
+    }
     if (kStage < 3) {
         for (int i = tid; i < kBins * kCopies; i += kChunkThreads) s_hist[i] = 0u;
         __syncthreads();
@@ -411,7 +424,7 @@ k_evict_move(CacheArgs c, CacheEvictArgs a, u32x4* K, u32x4* V, int chunks, int 
 size_t cache_evict_bytes(const CacheArgs& c) {
     if (c.L <= kKeysInLds) return 0;
     const size_t pairs = (size_t)c.batch * c.Hkv, chunks = ((size_t)c.L + kChunk - 1) / kChunk;
-    return (3 * pairs * kBins * sizeof(unsigned) + pairs * chunks * 2 * sizeof(int) + 255) / 256 * 256;
+    return (3 * pairs * (kBins + 2) * sizeof(unsigned) + pairs * chunks * 2 * sizeof(int) + 255) / 256 * 256;
 }
 
 // expects batch * Hkv <= 65535, sinks + recent <= keep, keep positions within the new table, and cache_evict_bytes() of workspace
@@ -429,7 +442,8 @@ hipError_t launch_cache_evict(const CacheArgs& c, int dtype, const CacheEvictArg
         sp.pairs = pairs;
         sp.chunks = (int)(((long long)c.L + kChunk - 1) / kChunk);
         sp.hist = reinterpret_cast<unsigned*>(workspace);
-        sp.count = reinterpret_cast<int*>(sp.hist + 3ll * pairs * kBins);
+        sp.pick = sp.hist + 3ll * pairs * kBins;
+        sp.count = reinterpret_cast<int*>(sp.pick + 6ll * pairs);
         const int pieces = 3 * pairs * kBins / 4;                       // (pairs <= 65535: below 2^27)
         hipLaunchKernelGGL(k_evict_clear, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, st, reinterpret_cast<u32x4*>(sp.hist), pieces);
         e = hipGetLastError();
