@@ -29,6 +29,6 @@ def __getattr__(name):
         import importlib
         binding = importlib.import_module(".binding", __name__)
         value = binding if name == "binding" else getattr(binding, name)
-        globals()[name] = value          # the next use finds it without this function (1.x us)
+        globals()[name] = value          # the next use finds it without this function
         return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

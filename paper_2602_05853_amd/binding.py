@@ -164,7 +164,7 @@ def make_shape(Q: torch.Tensor, K: torch.Tensor) -> rr_shape:
         raise RRError(RR_ERR_SHAPE)
     b, Hq, Lq, d = Q.shape
     kb, Hkv, L, kd = K.shape
-    if kb != b or kd != d or Lq > L:
+    if kb != b or kd != d or Lq > L or Lq < 1:          # (a length of 0 in the struct would be one of L)
         raise RRError(RR_ERR_SHAPE)
     return rr_shape(b, L, Hq, Hkv, d, _dtype_code(Q), q[0], q[1], q[2], k[0], k[1], k[2], Lq)
 
@@ -437,7 +437,7 @@ def rr_mask_from_dense(Q: torch.Tensor, K: torch.Tensor, dense: torch.Tensor, B:
 
 # The host's share of a short call: checks are plain comparisons of what torch hands out as it is (a device by its index, sizes as
 # torch.Size), the cache's struct is made once and again when one of its tensors is replaced or moves (one token for four short
-# sequences 13.8 -> 6.x us of Python, a step's write 12.6 -> 6.x).
+# sequences 13.8 -> 5.8 us of Python, a step's write 12.6 -> 4.4).
 
 def _on_device(index: int, *tensors) -> None:
     """Every tensor of a call lies on the one GPU the call runs on (-1: the CPU)."""
@@ -482,7 +482,26 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _bytes(t: Optional[torch.Tensor]) -> int:
-    return t.numel() * t.element_size() if t is not None else 0
+    if t is None:
+        return 0
+    if not t.is_contiguous():
+        raise RRError(RR_ERR_WORKSPACE)
+    return t.numel() * t.element_size()
+
+
+def _empty(shape, dtype: torch.dtype, like: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """Memory of the stream that the call runs on: what another stream has freed may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _output(Q: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    if stream is None:
+        return _output_like(Q)
+    with torch.cuda.stream(stream):
+        return _output_like(Q)
 
 
 def rr_window_workspace_bytes(Q: torch.Tensor, K: torch.Tensor, window: int, sinks: int = 0) -> int:
@@ -502,7 +521,7 @@ def rr_window_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, window: in
     if V.stride() != K.stride() or V.shape != K.shape:
         raise RRError(RR_ERR_SHAPE)
     if O is None:
-        O = _output_like(Q)
+        O = _output(Q, stream)
     else:
         _check_like(O, Q)
     if lse is not None:
@@ -545,8 +564,12 @@ class PagedCache:
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_made", None)          # the struct is of other tensors
 
+    def __getstate__(self):
+        return {**self.__dict__, "_made": None}          # addresses are no part of a copy
+
     def c_struct(self) -> rr_paged_cache:
-        """The cache's struct, its tensors checked against each other; kept until one of them is replaced or has moved."""
+        """The cache's struct, its tensors checked against each other; made again when one of them is replaced or has moved (a
+        tensor that is resized in place without moving still has the memory it had)."""
         K, V, table, length, weight = self.K, self.V, self.table, self.length, self.weight
         at = (K.data_ptr(), V.data_ptr(), weight.data_ptr() if weight is not None else None, table.data_ptr(), length.data_ptr())
         made = self._made
@@ -598,7 +621,7 @@ def rr_paged_attn(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: in
     shp = cache.shape(Q, Q.shape[1], max_length)
     flags = RR_FLAG_ACCUMULATE if accumulate else 0
     if O is None:
-        O = _output_like(Q)
+        O = _output(Q, stream)
     else:
         _check_like(O, Q)
     if lse is not None:
@@ -606,8 +629,7 @@ def rr_paged_attn(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: in
     index = Q.get_device()
     _on_device(index, cache.K, O, lse, workspace)
     if workspace is None:
-        workspace = torch.empty(lib.rr_paged_workspace_bytes(C.byref(shp), C.byref(c), window, sinks, flags), dtype=torch.uint8,
-                                device=Q.device)
+        workspace = _empty(lib.rr_paged_workspace_bytes(C.byref(shp), C.byref(c), window, sinks, flags), torch.uint8, Q, stream)
     _call(index, stream, lib.rr_paged_attn, C.byref(shp), Q.data_ptr(), C.byref(c), window, sinks, flags, O.data_ptr(), _ptr(lse),
           workspace.data_ptr(), _bytes(workspace))
     return O
@@ -647,14 +669,14 @@ def rr_key_weights(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, out: Opt
         raise RRError(RR_ERR_DTYPE)
     _check_array(lse, torch.float32, Q.shape[:3])
     if out is None:
-        out = torch.empty(K.shape[:3], dtype=torch.float32, device=K.device)
+        out = _empty(K.shape[:3], torch.float32, K, stream)
     else:
         _check_array(out, torch.float32, K.shape[:3])
     index = Q.get_device()
     _on_device(index, K, lse, out, workspace)
     if workspace is None:
         n = lib.rr_key_weights_workspace_bytes(C.byref(shp))
-        workspace = torch.empty(n, dtype=torch.uint8, device=Q.device) if n else None
+        workspace = _empty(n, torch.uint8, Q, stream) if n else None
     _call(index, stream, lib.rr_key_weights, C.byref(shp), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), out.data_ptr(),
           _ptr(workspace), _bytes(workspace))
     return out
@@ -686,18 +708,18 @@ def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int
         raise RRError(RR_ERR_SHAPE)
     _check_array(table, torch.int32, (batch, table.shape[1]))
     if length is None:
-        length = torch.empty(batch, dtype=torch.int32, device=K.device)
+        length = _empty(batch, torch.int32, K, stream)
     else:
         _check_array(length, torch.int32, (batch,))
     if kept is None:
-        kept = torch.empty((batch, Hkv, keep), dtype=torch.int32, device=K.device)
+        kept = _empty((batch, Hkv, keep), torch.int32, K, stream)
     else:
         _check_array(kept, torch.int32, (batch, Hkv, keep))
     index = K.get_device()
     _on_device(index, table, length, kept, workspace)
     if workspace is None:
         n = lib.rr_cache_evict_workspace_bytes(C.byref(shp), C.byref(c))
-        workspace = torch.empty(n, dtype=torch.uint8, device=K.device) if n else None
+        workspace = _empty(n, torch.uint8, K, stream) if n else None
     _call(index, stream, lib.rr_cache_evict, C.byref(shp), C.byref(c), keep, sinks, recent, table.data_ptr(), table.shape[1],
           length.data_ptr(), kept.data_ptr(), _ptr(workspace), _bytes(workspace))
     return PagedCache(cache.K, cache.V, table, length, cache.weight), kept

@@ -194,3 +194,36 @@ def test_binding_refusals():
     refused(bd.RR_ERR_PARAM, rr.rr_window_attn, q, k, k, 4, seq_first=torch.zeros(3, dtype=torch.int32))
     refused(bd.RR_ERR_PARAM, rr.rr_key_weights, q, k, torch.zeros(1, 4, 8))
     refused(bd.RR_ERR_SHAPE, rr.rr_key_weights, q, k, torch.zeros(1, 4, 9))
+    refused(bd.RR_ERR_SHAPE, rr.rr_window_attn, q[:, :, :0], k, k, 4)        # no queries
+    refused(bd.RR_ERR_SHAPE, rr.rr_key_weights, q[:, :, :0], k, torch.zeros(1, 4, 0))
+    refused(bd.RR_ERR_SHAPE, rr.rr_paged_attn, Q[:, :, :0], cache())
+
+
+def test_a_cache_follows_its_tensors():
+    """The struct of a cache is that of the tensors it has now, and no part of a copy."""
+    import copy
+    c = rr.PagedCache.allocate(8, 16, 2, 64, 3, 4, "cpu", weight=True)
+    s = c.c_struct()
+    assert (s.K, s.weight, s.page, s.num_pages, s.width) == (c.K.data_ptr(), c.weight.data_ptr(), 16, 8, 4) and c.c_struct() is s
+    c.table = torch.zeros(3, 5, dtype=torch.int32)
+    assert c.c_struct().width == 5 and c.c_struct().table == c.table.data_ptr()
+    c.weight = None
+    assert c.c_struct().weight is None
+    c.K.data, c.V.data = torch.zeros(9, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(9, 2, 16, 64, dtype=torch.bfloat16)
+    assert c.c_struct().num_pages == 9 and c.c_struct().K == c.K.data_ptr()
+    d = copy.deepcopy(c)
+    assert d.c_struct().K == d.K.data_ptr() != c.K.data_ptr()
+    c.length = torch.zeros(3)
+    refused(bd.RR_ERR_DTYPE, c.c_struct)
+
+
+def test_names_of_the_package():
+    """Every exported entry point is reachable from the package, also after a reload."""
+    import importlib
+    for name in ("rr_window_attn", "rr_window_workspace_bytes", "PagedCache", "rr_paged_attn", "rr_paged_workspace_bytes", "rr_paged_write",
+                 "rr_key_weights", "rr_key_weights_workspace_bytes", "rr_cache_evict", "rr_cache_evict_workspace_bytes"):
+        assert getattr(rr, name) is getattr(bd, name)
+    importlib.reload(rr)
+    assert "rr_paged_attn" not in vars(rr) and rr.rr_paged_attn is bd.rr_paged_attn and "rr_paged_attn" in vars(rr)
+    with pytest.raises(AttributeError):
+        rr.rr_no_such_name

@@ -86,6 +86,30 @@ def test_key_weights(dtype, Hq, Hkv, d, L, Lq):
     assert (err <= tol).all(), float((err / tol).max())
 
 
+@pytest.mark.parametrize("L,Lq,Hq,Hkv,batch", [(3000, 3000, 6, 2, 1), (5000, 40, 8, 2, 1), (2000, 700, 3, 1, 2), (700, 256, 2, 1, 1), (700, 288, 2, 1, 1)])
+def test_key_weights_of_longer_contexts(L, Lq, Hq, Hkv, batch):
+    """Tiles of keys shared by several workgroups, and one workgroup to a tile; every row gives one to its keys in all."""
+    g = torch.Generator(device=DEV).manual_seed(L)
+    Q = (torch.randn(batch, Hq, Lq, 128, generator=g, device=DEV) * 2).to(torch.bfloat16)
+    K = torch.randn(batch, Hkv, L, 128, generator=g, device=DEV).to(torch.bfloat16)
+    seen = sees(torch.arange(L - Lq, L, device=DEV), L, 0, 0)
+    lse = torch.empty(batch, Hq, Lq, device=DEV)
+    want = torch.zeros(batch, Hkv, L, dtype=torch.float64, device=DEV)
+    slack = torch.zeros_like(want)
+    for b in range(batch):
+        for h in range(Hq):
+            _, l, p, _, delta = attend(Q[b, h], K[b, h * Hkv // Hq], K[b, h * Hkv // Hq], seen)
+            lse[b, h] = l
+            want[b, h * Hkv // Hq] += p.sum(0)
+            slack[b, h * Hkv // Hq] += ((delta[:, None] + 4 * U32 * l.abs()[:, None] + 8 * U32) * p).sum(0)
+    n = rr.rr_key_weights_workspace_bytes(Q, K)
+    got = rr.rr_key_weights(Q, K, lse, workspace=torch.full((max(n, 256),), 0xFF, dtype=torch.uint8, device=DEV))
+    G = Hq // Hkv
+    tol = slack * 1.01 + (G * Lq + 8) * U32 * want + 1e-30
+    assert ((got.double() - want).abs() <= tol).all()
+    assert torch.equal(got, rr.rr_key_weights(Q, K, lse))
+
+
 def test_key_weights_of_rows_in_wider_tensors():
     big = torch.full((1, 150, 4, 80), math.nan, dtype=torch.bfloat16, device=DEV)
     Q, K = big[:, 10:60, 0:2, 8:72].transpose(1, 2), big[:, 20:120, 2:3, 8:72].transpose(1, 2)

@@ -106,6 +106,35 @@ def test_many_sequences():
     run(make(lengths, 1, 64, weight=True), 2, accumulate=True)
 
 
+@pytest.mark.parametrize("batch", [63, 64, 65, 256, 257])
+@pytest.mark.parametrize("d,dtype", [(128, torch.bfloat16), (64, torch.float32)])
+def test_numbers_of_sequences(batch, d, dtype):
+    """Around what a wave's lanes and a workgroup's threads hold; one long sequence last, so that the short ones share."""
+    run(make([(7 * i) % 33 for i in range(batch - 1)] + [1500], 1, d, dtype=dtype, weight=True), 2, accumulate=True)
+
+
+def test_memory_that_a_call_allocates_belongs_to_its_stream():
+    cache = make([3000, 100], 2, 128, weight=True)
+    Q = query(cache, 8)
+    want = rr.rr_paged_attn(Q, cache)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got = []
+    for _ in range(8):
+        got.append(rr.rr_paged_attn(Q, cache, stream=s))
+        torch.full((1 << 20,), math.nan, device=DEV)                         # what the current stream frees and fills is not the call's
+    s.synchronize()
+    assert all(torch.equal(want, g) for g in got)
+
+
+def test_a_workspace_with_gaps_is_refused():
+    cache = make([3000], 2, 128)
+    Q = query(cache, 8)
+    ws = torch.empty(2 * rr.rr_paged_workspace_bytes(Q, cache), dtype=torch.uint8, device=DEV)
+    with pytest.raises(rr.RRError):
+        rr.rr_paged_attn(Q, cache, workspace=ws[::2])
+
+
 def test_all_empty():
     cache = make([0, 0], weight=True)
     run(cache, 4, accumulate=True)
