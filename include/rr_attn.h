@@ -332,8 +332,9 @@ int rr_dense_attn_ws(const rr_shape* shape, const void* Q, const void* K, const 
  *              most 16 positions and 32 query rows per KV head then share the keys of a KV head out among several workgroups
  *              and read them once for all its query heads.  rr_window_workspace_bytes() is 0 for every other call, and for such
  *              steps that see few keys, which run that way without one.
- * Any L up to 2^30 (so have the caches below and rr_key_weights), d and strides of the conventions above.  bf16 with d = 128 (packed: B = 128) runs on a kernel of its own, which rounds
- * the probabilities to bf16; such steps and all other shapes hold nothing in fewer than 32 bits.  An infinite
+ * Any L up to 2^30 (so have the caches below and rr_key_weights), d and strides of the conventions above.  bf16 with d = 128 (packed: B = 128) and more than 128 blocks of 128 query
+ * rows over batch and heads runs on a kernel of its own, which rounds the probabilities to bf16; every other call holds nothing in
+ * fewer than 32 bits.  An infinite
  * or NaN value of V that no query of a launch's tile sees does not reach it; one that a query in the same tile sees makes the
  * channel NaN in that tile's other rows, as zero times infinity does.
  */

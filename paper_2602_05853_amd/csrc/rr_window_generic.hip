@@ -224,6 +224,10 @@ hipError_t launch_window_generic(const Geom& g, int dtype, const WindowArgs& a, 
             if (dtype == RR_BF16) {
                 if constexpr (N <= 4)
                     if (rows >= 64 * 512) return launch(k_window_generic<bf16_t, N, D, 4, 2, 4, 2>, 64, 4);
+                // (a few queries deep in a context end when the longest workgroup does: 16 queries on eight waves while those fill the
+                // chip once; d = 128, us, this / 32 on four waves: 100 of 24000, window 4096, 32 heads (224 workgroups) 42 / 53, 200
+                // (416) 80 / 55; 500, window 512, 8 heads (256) 11.0 / 15.1; 1024 positions, 8 heads (512) 19.8 / 19.4)
+                if (rows <= 16 * 256) return launch(k_window_generic<bf16_t, N, D, 1, 2, 8, 2>, 16, 8);
                 return launch(k_window_generic<bf16_t, N, D, 2, 2, 4, 2>, 32, 4);
             }
             // (1511 positions, 8 heads of 80, window 200, 95 tiles of 16 queries to a head, us: 16 queries on eight waves 20.0, on four

@@ -174,6 +174,8 @@ k_window_mfma(WindowKernelArgs ka) {
         __syncthreads();                                     // the buffers are free
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
+            const int h0 = 64 * hf;                          // a half that no query sees stays out
+            if (!(h0 < sinks || (h0 + 63 >= lo && h0 <= p_last - k0))) continue;
             // (no window reaches the block: the sinks' last row instead)
             const int first = lo > hi ? max(sinks - 1, 0) : max(lo, 0), last = lo > hi ? first : hi;
             issue_clamped(st, st.Kp, n, hf, st.k_dst(hf), false, sinks, first, last, lane);
@@ -242,8 +244,11 @@ bool window_mfma_takes(const Geom& g, int dtype, const int32_t* seq_first, int B
     if (dtype != RR_BF16 || g.d != 128 || (seq_first && B != 128)) return false;
     // a tile's rows are addressed by 32-bit byte offsets from its first
     if (g.ksl > (1ll << 23)) return false;
+    // A launch of few such rows ends when its longest does, and the generic kernel has four or eight times as many workgroups.  This
+    // kernel / that one, us: 512 positions, window 200, 32 heads (128 rows) 22.1 / 15.4; 2048, window 512, 8 heads (128) 24.3 / 21.9; 200
+    // of 24000, window 4096, 32 heads (64) 71 / 55, 500 (128 to 160) 73 / 87; 1024, 32 heads (256) 26.2 / 39.6.
     const long long rows = (long long)g.batch * g.Hq * ((g.L - 1) / 128 - g.q0 / 128 + 1);
-    return rows < (1ll << 23);
+    return rows > 128 && rows < (1ll << 23);
 }
 
 hipError_t launch_window_mfma(const Geom& g, const WindowArgs& a, hipStream_t st) {

@@ -17,14 +17,20 @@ def make(L, Lq, Hq=4, Hkv=2, d=128, dtype=torch.bfloat16, batch=1, seed=0):
     return t
 
 
-def check(Q, K, V, O, lse, window, sinks, start=None, rounded_p=None, rows=None):
+def matrix_kernel(Q, K):
+    """Whether a call without packed sequences runs on the kernel that rounds probabilities to bf16."""
+    (b, Hq, Lq, d), L = Q.shape, K.shape[2]
+    return Q.dtype == torch.bfloat16 and d == 128 and b * Hq * ((L - 1) // 128 - (L - Lq) // 128 + 1) > 128
+
+
+def check(Q, K, V, O, lse, window, sinks, start=None, rounded_p=None, rows=None, entries=None):
     (b, Hq, Lq, d), (Hkv, L) = Q.shape, K.shape[1:3]
     G = Hq // Hkv
     pos = torch.arange(L - Lq, L, device=DEV)
     rows = torch.arange(Lq, device=DEV) if rows is None else rows
     seen = sees(pos[rows], L, window, sinks, 0 if start is None else start[rows])
-    rounded = Q.dtype == torch.bfloat16 and d == 128 if rounded_p is None else rounded_p
-    for i in range(b):
+    rounded = matrix_kernel(Q, K) if rounded_p is None else rounded_p
+    for i in range(b) if entries is None else entries:
         for h in range(Hq):
             check_rows(O[i, h, rows], None if lse is None else lse[i, h, rows], Q[i, h, rows], K[i, h // G], V[i, h // G], seen, rounded,
                        what=(i, h))
@@ -52,6 +58,57 @@ def test_lengths_windows_and_sinks(d, L, Lq, window, sinks):
     run(L, Lq, window, sinks, d=d)
 
 
+@pytest.mark.parametrize("L,Lq", [(1, 1), (127, 127), (128, 128), (129, 129), (1000, 1000), (1000, 20), (1000, 129), (700, 333), (640, 256)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (17, 0), (64, 70), (128, 0), (129, 4), (300, 128), (256, 260), (513, 64), (100000, 0), (90, 100000)])
+def test_matrix_kernel(L, Lq, window, sinks):
+    """bf16, d = 128, on more than 128 query blocks: the first and the last entry of a batch that has as many."""
+    blocks = (L - 1) // 128 - (L - Lq) // 128 + 1
+    batch = 128 // (4 * blocks) + 1
+    Q, K, V = make(L, Lq, batch=batch)
+    step = rr.rr_window_workspace_bytes(Q, K, window, sinks) > 0 or (Lq <= 16 and min(window, L) + sinks < 400)
+    assert matrix_kernel(Q, K) or step
+    lse = torch.full(Q.shape[:3], 5.0, device=DEV)
+    O = rr.rr_window_attn(Q, K, V, window, sinks, lse=lse)
+    check(Q, K, V, O, lse, window, sinks, entries=[0, batch - 1])
+
+
+def test_matrix_kernel_of_values_that_nobody_sees_and_one_that_is_infinite():
+    Q, K, V = make(900, 40, batch=17)
+    window, sinks = 60, 5
+    gap = slice(sinks, 900 - 40 - window + 1)
+    K[:, :, gap], V[:, :, gap] = math.nan, math.inf
+    lse = torch.empty(Q.shape[:3], device=DEV)
+    O = rr.rr_window_attn(Q, K, V, window, sinks, lse=lse)
+    assert matrix_kernel(Q, K)
+    check(Q, K, V, O, lse, window, sinks, entries=[0, 16])
+    Q, K, V = make(600, 600, Hq=2, Hkv=1, batch=13)
+    assert matrix_kernel(Q, K)
+    V[3, 0, 200, 7] = math.inf
+    O = rr.rr_window_attn(Q, K, V, 100, 0)
+    assert (O[3, :, 200:300, 7] == math.inf).all()
+    O[3, :, 128:384, 7] = 0
+    assert O.isfinite().all()
+
+
+def test_matrix_kernel_strides_and_what_lies_beside():
+    g = torch.Generator(device=DEV).manual_seed(2)
+
+    def inside(n, heads, fill):
+        big = torch.full((9, n + 2, heads + 1, 144), fill, dtype=torch.bfloat16, device=DEV)
+        return big, big[:, 1:n + 1, :heads, 8:136].transpose(1, 2)
+    bigs, views = zip(*(inside(n, h, math.nan) for n, h in ((200, 8), (300, 2), (300, 2))))
+    for v in views:
+        v.copy_(torch.randn(v.shape, generator=g, device=DEV))
+    Q, K, V = views
+    assert matrix_kernel(Q, K)
+    out, O = inside(200, 8, 3.0)
+    lse = torch.empty(Q.shape[:3], device=DEV)
+    rr.rr_window_attn(Q, K, V, 77, 9, O=O, lse=lse)
+    check(Q, K, V, O, lse, 77, 9, entries=[0, 8])
+    O.fill_(3.0)
+    assert (out == 3.0).all()
+
+
 @pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 128)])
 def test_a_window_over_everything_is_dense(dtype, d):
     Q, K, V, O, lse = run(500, 500, 2 ** 31 - 1, 2 ** 31 - 1, dtype=dtype, d=d)
@@ -74,7 +131,7 @@ def test_longer_prompts(L, window, sinks):
 def test_packed_sequences(dtype, d, B, window, sinks):
     blocks = [3, 1, 1, 7, 2, 4]
     L = B * sum(blocks) - 9
-    Q, K, V = make(L, L, d=d, dtype=dtype, batch=2)
+    Q, K, V = make(L, L, d=d, dtype=dtype, batch=2, Hq=8)
     sf = rr.packed_seq_first(blocks, DEV)
     lse = torch.empty(Q.shape[:3], device=DEV)
     O = rr.rr_window_attn(Q, K, V, window, sinks, lse=lse, seq_first=sf, B=B)
@@ -139,7 +196,8 @@ def test_one_infinite_value_reaches_the_rows_that_see_it():
 
 
 def test_captured_and_replayed():
-    Q, K, V = make(700, 700, Hq=8, Hkv=2)
+    Q, K, V = make(700, 700, Hq=24, Hkv=2)                    # 144 query blocks: the matrix kernel
+    assert matrix_kernel(Q, K)
     step = Q[:, :, -1:].contiguous()
     ws = torch.empty(rr.rr_window_workspace_bytes(step, K, 300, 4), dtype=torch.uint8, device=DEV)
     O, S = torch.empty_like(Q), torch.empty_like(step)
@@ -160,7 +218,8 @@ def test_captured_and_replayed():
 
 
 def test_batch_on_another_stream():
-    Q, K, V = make(400, 400, batch=3)
+    Q, K, V = make(400, 400, batch=12)
+    assert matrix_kernel(Q, K)
     want = rr.rr_window_attn(Q, K, V, 128, 4)
     torch.cuda.synchronize()
     s = torch.cuda.Stream()
