@@ -275,20 +275,22 @@ k_cache_attn(CacheArgs c) {
 }
 
 // One workgroup per query row: O = sum_p w_p O_p / sum_p w_p with w_p = 2^(lse_p - max), rounded once.
-// A wave takes every fourth part, eight requested at once: one at a time their latencies were the kernel (64 parts 15 us).
-template <typename T>
-__global__ void __launch_bounds__(256)
+// A wave takes every KW-th part, eight requested at once, the first eight in front of everything that waits: one at a time, after the
+// weights, their latencies were the kernel (64 parts 15.4 us, so 5.4).
+template <typename T, int KW>
+__global__ void __launch_bounds__(64 * KW)
 k_cache_join(CacheArgs c, int row_tile, int workgroups) {
-    __shared__ Shares<256> s_shares;
+    constexpr int kThreads = 64 * KW, kAtOnce = 8;
+    __shared__ Shares<kThreads> s_shares;
     __shared__ float s_w[kCacheWorkgroups];
-    __shared__ float s_red[4], s_den[4];
-    __shared__ __align__(16) float s_o[4][256];
+    __shared__ float s_red[KW], s_den[KW];
+    __shared__ __align__(16) float s_o[KW][256];
     const float NEG_INF = -__builtin_huge_valf();
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = c.G * c.T, pairs = c.Hkv * c.row_tiles;
     const int row = blockIdx.x;                          // (b, kv, r)
-    const int r = row % R, kv = row / R % c.Hkv, b = row / R / c.Hkv;
-    const int pair = kv * c.row_tiles + r / row_tile;
+    const int bk = row / R, r = row - bk * R, b = bk / c.Hkv, kv = bk - b * c.Hkv;
+    const int rt = c.row_tiles == 1 ? 0 : r / row_tile, in_tile = r - rt * row_tile, pair = kv * c.row_tiles + rt;
 
     int upto;
     const int total = shares_scan(c, s_shares, upto);
@@ -302,11 +304,24 @@ k_cache_join(CacheArgs c, int row_tile, int workgroups) {
         parts = (int)(deal.owner(u + (unsigned)v.n - 1) - (unsigned)first) + 1;
     }
     const long long slot = first + (long long)b * pairs + pair;
-    const float* lse = c.part_lse + slot * row_tile + r % row_tile;
-    const float* O = c.part_O + (slot * row_tile + r % row_tile) * c.d;
+    const float* lse = c.part_lse + slot * row_tile + in_tile;
+    const float* O = c.part_O + (slot * row_tile + in_tile) * c.d;
 
+    // a lane has the channels 2 lane, 2 lane + 1, and the two 128 behind them
+    const int ch = 2 * lane;
+    float2 x[kAtOnce][2];
+    auto request = [&](int p0) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (p0 + KW * i >= parts) break;             // (the same in every lane)
+            const float* at = O + (long long)(p0 + KW * i) * row_tile * c.d;
+            x[i][0] = *reinterpret_cast<const float2*>(at + (ch < c.d ? ch : 0));
+            if (c.d > 128) x[i][1] = *reinterpret_cast<const float2*>(at + (128 + ch < c.d ? 128 + ch : 0));
+        }
+    };
+    request(wv);
     float mx = NEG_INF;
-    for (int p = tid; p < parts; p += 256) {
+    for (int p = tid; p < parts; p += kThreads) {
         const float l = lse[(long long)p * row_tile];
         s_w[p] = l;
         mx = fmaxf(mx, l);
@@ -314,24 +329,18 @@ k_cache_join(CacheArgs c, int row_tile, int workgroups) {
     mx = wave_max(mx);
     if (lane == 0) s_red[wv] = mx;
     __syncthreads();
-    mx = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+    mx = s_red[0];
+#pragma unroll
+    for (int i = 1; i < KW; ++i) mx = fmaxf(mx, s_red[i]);
 
-    // a lane has the channels 2 lane, 2 lane + 1, and the two 128 behind them
-    const int ch = 2 * lane;
     float den = 0.f;
     float2 o[2] = {{0.f, 0.f}, {0.f, 0.f}};
-    auto take = [&](int p0, auto n) {
-        constexpr int N = decltype(n)::value;
-        float2 x[N][2];
+    for (int p0 = wv; p0 < parts; p0 += KW * kAtOnce) {
+        if (p0 != wv) request(p0);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float* at = O + (long long)min(p0 + 4 * i, parts - 1) * row_tile * c.d;
-            x[i][0] = *reinterpret_cast<const float2*>(at + (ch < c.d ? ch : 0));
-            if (c.d > 128) x[i][1] = *reinterpret_cast<const float2*>(at + (128 + ch < c.d ? 128 + ch : 0));
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float l = p0 + 4 * i < parts ? s_w[p0 + 4 * i] : NEG_INF;
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (p0 + KW * i >= parts) break;
+            const float l = s_w[p0 + KW * i];
             if (l == NEG_INF) continue;                  // (whatever it holds)
             const float wp = __builtin_amdgcn_exp2f(l - mx);
             den += wp;
@@ -342,11 +351,7 @@ k_cache_join(CacheArgs c, int row_tile, int workgroups) {
                 o[1].y = fmaf(wp, x[i][1].y, o[1].y);
             }
         }
-    };
-    int p0 = wv;
-    for (; p0 + 16 < parts; p0 += 32) take(p0, std::integral_constant<int, 8>{});
-    if (p0 + 4 < parts) { take(p0, std::integral_constant<int, 4>{}); p0 += 16; }
-    if (p0 < parts) take(p0, std::integral_constant<int, 1>{});
+    }
     if (lane == 0) s_den[wv] = den;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -354,16 +359,17 @@ k_cache_join(CacheArgs c, int row_tile, int workgroups) {
         s_o[wv][128 * k + ch + 1] = o[k].y;
     }
     __syncthreads();
-    den = (s_den[0] + s_den[1]) + (s_den[2] + s_den[3]);
-    const float inv = den > 0.f ? 1.0f / den : 0.f;
-    const int hl = r / c.T, tk = r - hl * c.T, h = kv * c.G + hl;
-    if (4 * tid < c.d) {
-        f32x4 sum;
+    den = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = 4 * tid + e;
-            sum[e] = ((s_o[0][i] + s_o[1][i]) + (s_o[2][i] + s_o[3][i])) * inv;
-        }
+    for (int i = 0; i < KW; ++i) den += s_den[i];
+    const float inv = den > 0.f ? 1.0f / den : 0.f;
+    const int hl = c.T == 1 ? r : r / c.T, tk = r - hl * c.T, h = kv * c.G + hl;
+    if (4 * tid < c.d) {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < KW; ++i) sum += *reinterpret_cast<const f32x4*>(&s_o[i][4 * tid]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] *= inv;
         store4(reinterpret_cast<T*>(c.O) + b * c.qsb + h * c.qsh + tk * c.qsl + 4 * tid, sum);
     }
     if (tid == 0) {
@@ -491,8 +497,13 @@ hipError_t launch_cache_attn(const CacheArgs& c, int dtype, const CachePlan& pla
     if (e != hipSuccess) return e;
     if (!plan.whole) {
         const dim3 rows((unsigned)(c.batch * c.Hkv * c.G * c.T));
-        if (dtype == RR_BF16) hipLaunchKernelGGL(k_cache_join<bf16_t>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
-        else hipLaunchKernelGGL(k_cache_join<float>, rows, dim3(256), 0, st, c, plan.row_tile, plan.workgroups);
+        // (rows of few parts on four waves: 64 uneven sequences, 2048 rows of two or three parts)
+        auto join = [&](auto kernel, int waves) {
+            hipLaunchKernelGGL(kernel, rows, dim3(64 * waves), 0, st, c, plan.row_tile, plan.workgroups);
+        };
+        const bool many = plan.workgroups > 16ll * c.batch * c.Hkv * c.row_tiles;
+        if (dtype == RR_BF16) many ? join(k_cache_join<bf16_t, 8>, 8) : join(k_cache_join<bf16_t, 4>, 4);
+        else many ? join(k_cache_join<float, 8>, 8) : join(k_cache_join<float, 4>, 4);
         e = hipGetLastError();
     }
     if (e != hipSuccess || !c.scores) return e;
