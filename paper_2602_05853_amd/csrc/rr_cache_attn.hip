@@ -173,13 +173,16 @@ k_cache_attn(CacheArgs c) {
                                        (key0[tl] > q_last - c.window || key0[tl] + 15 < c.sinks);
                     if (!whole) {
 #pragma unroll
-                        for (int t = 0; t < QT; ++t)
+                        for (int t = 0; t < QT; ++t) {
+                            f32x4 x4 = s[t][tl];
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const int k = 4 * gq + r, key = key0[tl] + k;
                                 const bool sees = k <= last[tl] && key <= qpos[t] && (key > qpos[t] - c.window || key < c.sinks);
-                                s[t][tl][r] = sees ? s[t][tl][r] : NEG_INF;
+                                x4[r] = sees ? x4[r] : NEG_INF;
                             }
+                            s[t][tl] = x4;
+                        }
                     }
                     if (c.scores) {
                         const int rows = min(R, kQ);
