@@ -7,6 +7,10 @@
 // the sinks end in.  What bounds it: the matrix pipe (4 d operations a visible pair); the partial blocks, three or four at most, cost
 // about twice a whole one, a window of 4096 positions has 31 of those.
 //
+// Not taken (us, 8192 tokens, 32 / 8 heads; windows of 128, 256, 512, 1000: 73, 82, 106, 163): the masked tiles staged a half ahead of their
+// use 77, 87, 111, 171; 32 positions of a KV group's four heads to a workgroup, whose windows differ by less, 66, 93, 122, 185 (every
+// wave then meets every masked key, where with 128 positions a wave skips most of those that are not its queries').
+//
 // Rows are dealt to the XCDs in eight runs, group after group, the heads of a group next to each other and then the query blocks:
 // rows that run on an XCD at the same time then walk nearly the same window (2 MB of K and V for 4096 positions) in its 4 MB of L2.
 //
@@ -201,9 +205,9 @@ k_window_mfma(WindowKernelArgs ka) {
             pv_step(w, j >> 1, j & 1, pa);
         }
     };
-    if (sink_part) partial_block(f + n_sink);
-    for (int n = w_any; n < w_full; ++n) partial_block(n);
-    partial_block(m);
+    // (one loop, so that the pass is there once: 12700 instructions so, 6400)
+    const int in_front = sink_part ? 1 : 0, partial = in_front + w_full - w_any + 1;
+    for (int i = 0; i < partial; ++i) partial_block(i < in_front ? f + n_sink : i + 1 < partial ? w_any + i - in_front : m);
     __syncthreads();
 
     // ---- normalise, write ----

@@ -60,28 +60,27 @@ def test_lengths_windows_and_sinks(d, L, Lq, window, sinks):
 
 @pytest.mark.parametrize("L,Lq", [(1, 1), (127, 127), (128, 128), (129, 129), (1000, 1000), (1000, 20), (1000, 129), (700, 333), (640, 256)])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (17, 0), (64, 70), (128, 0), (129, 4), (300, 128), (256, 260), (513, 64), (100000, 0), (90, 100000)])
-def test_matrix_kernel(L, Lq, window, sinks):
+@pytest.mark.parametrize("Hq,Hkv", [(4, 4), (8, 2), (14, 2)])
+def test_matrix_kernel(Hq, Hkv, L, Lq, window, sinks):
     """bf16, d = 128, on more than 128 query blocks: the first and the last entry of a batch that has as many."""
-    blocks = (L - 1) // 128 - (L - Lq) // 128 + 1
-    batch = 128 // (4 * blocks) + 1
-    Q, K, V = make(L, Lq, batch=batch)
-    step = rr.rr_window_workspace_bytes(Q, K, window, sinks) > 0 or (Lq <= 16 and min(window, L) + sinks < 400)
-    assert matrix_kernel(Q, K) or step
+    batch = 128 // (Hq * ((L - 1) // 128 - (L - Lq) // 128 + 1)) + 1
+    Q, K, V = make(L, Lq, Hq=Hq, Hkv=Hkv, batch=batch)
+    assert matrix_kernel(Q, K)
     lse = torch.full(Q.shape[:3], 5.0, device=DEV)
     O = rr.rr_window_attn(Q, K, V, window, sinks, lse=lse)
     check(Q, K, V, O, lse, window, sinks, entries=[0, batch - 1])
 
 
 def test_matrix_kernel_of_values_that_nobody_sees_and_one_that_is_infinite():
-    Q, K, V = make(900, 40, batch=17)
+    Q, K, V = make(900, 40, batch=65)
     window, sinks = 60, 5
     gap = slice(sinks, 900 - 40 - window + 1)
     K[:, :, gap], V[:, :, gap] = math.nan, math.inf
     lse = torch.empty(Q.shape[:3], device=DEV)
     O = rr.rr_window_attn(Q, K, V, window, sinks, lse=lse)
     assert matrix_kernel(Q, K)
-    check(Q, K, V, O, lse, window, sinks, entries=[0, 16])
-    Q, K, V = make(600, 600, Hq=2, Hkv=1, batch=13)
+    check(Q, K, V, O, lse, window, sinks, entries=[0, 64])
+    Q, K, V = make(600, 600, Hq=2, Hkv=1, batch=14)
     assert matrix_kernel(Q, K)
     V[3, 0, 200, 7] = math.inf
     O = rr.rr_window_attn(Q, K, V, 100, 0)
@@ -94,7 +93,7 @@ def test_matrix_kernel_strides_and_what_lies_beside():
     g = torch.Generator(device=DEV).manual_seed(2)
 
     def inside(n, heads, fill):
-        big = torch.full((9, n + 2, heads + 1, 144), fill, dtype=torch.bfloat16, device=DEV)
+        big = torch.full((10, n + 2, heads + 1, 144), fill, dtype=torch.bfloat16, device=DEV)
         return big, big[:, 1:n + 1, :heads, 8:136].transpose(1, 2)
     bigs, views = zip(*(inside(n, h, math.nan) for n, h in ((200, 8), (300, 2), (300, 2))))
     for v in views:
@@ -104,7 +103,7 @@ def test_matrix_kernel_strides_and_what_lies_beside():
     out, O = inside(200, 8, 3.0)
     lse = torch.empty(Q.shape[:3], device=DEV)
     rr.rr_window_attn(Q, K, V, 77, 9, O=O, lse=lse)
-    check(Q, K, V, O, lse, 77, 9, entries=[0, 8])
+    check(Q, K, V, O, lse, 77, 9, entries=[0, 9])
     O.fill_(3.0)
     assert (out == 3.0).all()
 
