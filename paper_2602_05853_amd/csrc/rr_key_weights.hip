@@ -21,7 +21,10 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kRows = 32;                                       // query rows to a stage
-constexpr int kWholeTiles = 16;                                 // tiles of at most so many stages are not split
+// Tiles of at most so many stages are not split, where they give the chip a workgroup to each compute unit, or are short.  (Split, the
+// shares of at least two stages; us: 100 positions, 32 / 8 heads 21.7 whole, 14.6 split; fp32, 100 rows of 1000, 8 / 2 heads 44.4, 14.5;
+// 32 rows of 2000, 32 / 8 heads 10.6, 15.0; 64 rows of 64K 60, 68.)
+constexpr int kWholeStages = 16, kShortStages = 4, kManyTiles = 256;
 
 // Pairs of 16-key tiles that a wave holds: 64 keys where they take 64 registers or fewer.
 template <typename T, int NT> constexpr int pairs_of() {
@@ -233,14 +236,15 @@ Stages stages_of(const Geom& g, int dtype) {
     s.per_tile = keys / kRows;
     s.c0 = (g.q0 + kRows - 1) / kRows;
     s.per_pair = s.before(s.tiles);
-    s.whole = (long long)g.G * s.per_head <= kWholeTiles;
+    s.whole = (long long)g.G * s.per_head <= ((long long)g.batch * g.Hkv * s.tiles >= kManyTiles ? kWholeStages : kShortStages);
     return s;
 }
-// One round of workgroups, each of at least four stages where there are as many
+// One round of workgroups, of at least two stages each and no more workgroups than finish as early
 int workgroups_of(const Geom& g, const Stages& s, int occupancy) {
     const long long tiles = (long long)g.batch * g.Hkv * s.tiles, U = s.per_pair * g.batch * g.Hkv;
     if (s.whole) return (int)tiles;
-    return (int)std::max(1ll, std::min(256ll * occupancy, U / 4));
+    const long long each = std::max(2ll, (U + 256 * occupancy - 1) / (256 * occupancy));
+    return (int)((U + each - 1) / each);
 }
 constexpr int kMostOccupancy = 3;
 
