@@ -465,6 +465,13 @@ def _call(index: int, stream: Optional[torch.cuda.Stream], entry, *args) -> None
         raise RRError(status)
 
 
+def _check_ints(*values: int) -> None:
+    """ctypes takes the low 32 bits of a larger number without a word."""
+    for v in values:
+        if not -0x80000000 <= v <= 0x7fffffff:
+            raise RRError(RR_ERR_PARAM)
+
+
 def _check_like(t: torch.Tensor, like: torch.Tensor) -> None:
     if t.shape != like.shape or t.stride() != like.stride() or t.dtype != like.dtype:
         raise RRError(RR_ERR_SHAPE)
@@ -506,6 +513,7 @@ def _output(Q: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> torch.Tenso
 
 def rr_window_workspace_bytes(Q: torch.Tensor, K: torch.Tensor, window: int, sinks: int = 0) -> int:
     """Bytes of scratch with which rr_window_attn shares a step's keys out among workgroups (0: it does without)."""
+    _check_ints(window, sinks)
     return lib.rr_window_workspace_bytes(C.byref(make_shape(Q, K)), window, sinks)
 
 
@@ -516,6 +524,7 @@ def rr_window_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, window: in
     """Causal attention with a sliding window of `window` positions, the first `sinks` ones always visible.  seq_first, B:
     packed sequences, as for rr_dense_attn_packed."""
     shp = make_shape(Q, K)
+    _check_ints(window, sinks, B)
     if K.dtype != Q.dtype or V.dtype != Q.dtype:
         raise RRError(RR_ERR_DTYPE)
     if V.stride() != K.stride() or V.shape != K.shape:
@@ -601,12 +610,13 @@ class PagedCache:
             raise RRError(RR_ERR_SHAPE)
         if rows.dtype is not K.dtype:
             raise RRError(RR_ERR_DTYPE)
-        return rr_shape(batch, width * of_pool[2] if max_length is None else max_length, Hq, of_pool[1], of_pool[3], _dtype_code(K),
+        return rr_shape(batch, min(width * of_pool[2], 1 << 30) if max_length is None else max_length, Hq, of_pool[1], of_pool[3], _dtype_code(K),
                         r[0], r[1], r[2], k[0], k[1], k[2], of_rows[2])
 
 
 def rr_paged_workspace_bytes(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: int = 0, accumulate: bool = False,
                              max_length: Optional[int] = None) -> int:
+    _check_ints(window, sinks, max_length or 0)
     c = cache.c_struct()
     shp = cache.shape(Q, Q.shape[1], max_length)
     return lib.rr_paged_workspace_bytes(C.byref(shp), C.byref(c), window, sinks, RR_FLAG_ACCUMULATE if accumulate else 0)
@@ -617,6 +627,7 @@ def rr_paged_attn(Q: torch.Tensor, cache: PagedCache, window: int = 0, sinks: in
                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Attention of the last Lq positions of every sequence, Q [batch, Hq, Lq, d], against the cache.  max_length: the most
     positions a sequence has (default: what the table holds).  Without `workspace` one is allocated."""
+    _check_ints(window, sinks, max_length or 0)
     c = cache.c_struct()
     shp = cache.shape(Q, Q.shape[1], max_length)
     flags = RR_FLAG_ACCUMULATE if accumulate else 0
@@ -690,7 +701,7 @@ def _pool_shape(cache: PagedCache) -> rr_shape:
     """(no rows of queries belong to the call: the pool's own layout in their place)"""
     K = cache.K
     (batch, width), (_, Hkv, page, d), k = cache.table.shape, K.shape, K.stride()
-    return rr_shape(batch, width * page, Hkv, Hkv, d, _dtype_code(K), k[0], k[1], k[2], k[0], k[1], k[2], 1)
+    return rr_shape(batch, min(width * page, 1 << 30), Hkv, Hkv, d, _dtype_code(K), k[0], k[1], k[2], k[0], k[1], k[2], 1)
 
 
 def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int = 0, recent: int = 0,
@@ -702,6 +713,7 @@ def rr_cache_evict(cache: PagedCache, table: torch.Tensor, keep: int, sinks: int
     c = cache.c_struct()
     K, shp = cache.K, _pool_shape(cache)
     batch, Hkv = shp.batch, shp.Hkv
+    _check_ints(keep, sinks, recent)
     if keep < 1:
         raise RRError(RR_ERR_PARAM)
     if table.dim() != 2:

@@ -17,7 +17,7 @@ typedef const int32_t* scalar_words_t;                                     // th
 
 // position / page.  Pages are multiples of 16, so n = position / 16 < 2^27 is divided by p = page / 16: with l the bits of p - 1,
 // s = 27 + l and M = ceil(2^s / p) <= 2^28, M p - 2^s < p <= 2^l, so n (M p - 2^s) < 2^s and n M / 2^s has the quotient as its
-// whole part.  (A 32-bit division is some forty vector instructions: they were half of a sweep over a long cache's weights.)
+// whole part.  (A 32-bit division is some forty vector instructions.)
 inline void set_page(CacheArgs* c, int page) {
     c->page = page;
     const unsigned p = (unsigned)page >> 4;

@@ -13,6 +13,11 @@
 //
 // Weights: the first kernel also keeps its scores (4 bytes per row and key against the 4 d and 8 d of a key's K and V), and a
 // third adds exp(score - lse) over the rows of a KV head, in the order of the rows, to the positions' sums.
+//
+// Measured (bf16, 32 / 8 heads of 128): one token over 128K positions 96 us (5.6 TB/s) and 5.8 to join; 64 sequences of 200 to 16384,
+// pages of 16, 442 + 9 + 27 us (the first at 4.9 TB/s); a step over a window of 8192 11.4 + 4.6 us.  Tried and not kept: the values of
+// the next step requested with its keys (no change), three workgroups to a compute unit (128 us, spills), runs of shares to an XCD
+// (no change, short steps 17.4 -> 19.7).
 #include "rr_cache.hpp"
 #include "rr_attn_frag.hpp"
 

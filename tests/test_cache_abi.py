@@ -199,6 +199,23 @@ def test_binding_refusals():
     refused(bd.RR_ERR_SHAPE, rr.rr_paged_attn, Q[:, :, :0], cache())
 
 
+def test_numbers_that_32_bits_do_not_hold():
+    """ctypes would take their low bits."""
+    q, k = torch.zeros(1, 4, 8, 64), torch.zeros(1, 2, 8, 64)
+    c = rr.PagedCache.allocate(8, 16, 2, 64, 3, 4, "cpu", weight=True)
+    Q = torch.zeros(3, 4, 1, 64, dtype=torch.bfloat16)
+    for big in (2 ** 31, 2 ** 32 + 5, -2 ** 31 - 1):
+        refused(bd.RR_ERR_PARAM, rr.rr_window_attn, q, k, k, big)
+        refused(bd.RR_ERR_PARAM, rr.rr_window_attn, q, k, k, 4, big)
+        refused(bd.RR_ERR_PARAM, rr.rr_window_workspace_bytes, q, k, big)
+        refused(bd.RR_ERR_PARAM, rr.rr_paged_attn, Q, c, big)
+        refused(bd.RR_ERR_PARAM, rr.rr_paged_attn, Q, c, 0, big)
+        refused(bd.RR_ERR_PARAM, rr.rr_paged_attn, Q, c, max_length=big)
+        refused(bd.RR_ERR_PARAM, rr.rr_paged_workspace_bytes, Q, c, big)
+        refused(bd.RR_ERR_PARAM, rr.rr_cache_evict, c, torch.zeros(3, 2, dtype=torch.int32), big)
+        refused(bd.RR_ERR_PARAM, rr.rr_cache_evict, c, torch.zeros(3, 2, dtype=torch.int32), 20, big)
+
+
 def test_a_cache_follows_its_tensors():
     """The struct of a cache is that of the tensors it has now, and no part of a copy."""
     import copy

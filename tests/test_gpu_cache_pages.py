@@ -221,6 +221,40 @@ def test_evict_into_its_own_length():
     assert new.length is cache.length and cache.length.tolist() == [80, 20]
 
 
+def test_a_captured_prompt_and_step():
+    """Key weights, a write with them, a step's write and its attention in one graph, replayed on new inputs; two workspaces shared."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    cache = make([500], 2, 128, 16, weight=True)
+    Q, K = torch.empty(1, 8, 500, 128, dtype=torch.bfloat16, device=DEV), torch.empty(1, 2, 500, 128, dtype=torch.bfloat16, device=DEV)
+    lse, first = torch.empty(1, 8, 500, device=DEV), torch.empty(1, 2, 500, device=DEV)
+    q, O = torch.empty(1, 8, 1, 128, dtype=torch.bfloat16, device=DEV), torch.empty(1, 8, 1, 128, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(max(rr.rr_key_weights_workspace_bytes(Q, K), rr.rr_paged_workspace_bytes(q, cache, accumulate=True)), dtype=torch.uint8, device=DEV)
+
+    def fill():
+        for x in (Q, K, q):
+            x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        rr.rr_window_attn(Q, K, K, 500, 0, lse=lse)
+
+    def work():
+        rr.rr_key_weights(Q, K, lse, out=first, workspace=ws)
+        rr.rr_paged_write(cache, K, K, weight=first)
+        rr.rr_paged_attn(q, cache, accumulate=True, O=O, workspace=ws)
+    fill()
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for _ in range(4):
+        fill()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = O.clone(), first.clone(), cache.weight.clone()
+        work()
+        assert torch.equal(got[0], O) and torch.equal(got[1], first) and torch.equal(got[2], cache.weight)
+        assert abs(float(first.sum()) - 8 * 500) < 0.1
+
+
 def test_evict_captured():
     cache = make([700, 90], 2, 64, weight=True, spare=30)
     used = set(cache.table.flatten().tolist())
