@@ -332,11 +332,11 @@ int rr_dense_attn_ws(const rr_shape* shape, const void* Q, const void* K, const 
  *              most 16 positions and 32 query rows per KV head then share the keys of a KV head out among several workgroups
  *              and read them once for all its query heads.  rr_window_workspace_bytes() is 0 for every other call, and for such
  *              steps that see few keys, which run that way without one.
- * Any L up to 2^30 (so have the caches below and rr_key_weights), d and strides of the conventions above.  bf16 with d = 128 (packed: B = 128) and more than 128 blocks of 128 query
- * rows over batch and heads runs on a kernel of its own, which rounds the probabilities to bf16; every other call holds nothing in
- * fewer than 32 bits.  An infinite
- * or NaN value of V that no query of a launch's tile sees does not reach it; one that a query in the same tile sees makes the
- * channel NaN in that tile's other rows, as zero times infinity does.
+ * Any L up to 2^30 (so have the caches below and rr_key_weights), d and strides of the conventions above.  bf16 with d = 128
+ * (packed: B = 128) and more than 128 blocks of 128 query rows over batch and heads runs on a kernel of its own, which rounds the
+ * probabilities to bf16; every other call holds nothing in fewer than 32 bits.  lse is that of the unrounded probabilities.
+ * An infinite or NaN value of V that no query of a launch's tile sees does not reach it; one that a query in the same tile sees
+ * makes the channel NaN in that tile's other rows, as zero times infinity does.
  */
 size_t rr_window_workspace_bytes(const rr_shape* shape, int window, int sinks);
 int rr_window_attn(const rr_shape* shape, const void* Q, const void* K, const void* V, int window, int sinks,
@@ -348,8 +348,8 @@ int rr_window_attn(const rr_shape* shape, const void* Q, const void* K, const vo
  * sequence b lies in page table[b][p / page] at slot p % page.  K and V are pools of pages addressed as
  * base + page*kv_stride_b + h*kv_stride_h + slot*kv_stride_l + c with the strides of the rr_shape of the call (so both
  * [pages, Hkv, page, d] and [pages, page, Hkv, d] are possible).
- *   weight     [num_pages, Hkv, page] fp32 contiguous, 16-byte aligned: what every position's key has got of softmax weights so far.  May be NULL
- *              where nothing reads or writes it.
+ *   weight     [num_pages, Hkv, page] fp32 contiguous, 16-byte aligned: what every position's key has got of softmax weights so
+ *              far.  May be NULL where nothing reads or writes it.
  *   table      [batch, width] int32.  An entry outside [0, num_pages) is no page: its positions hold nothing, are attended by
  *              nobody and are not written.
  *   length     [batch] int32: positions of every sequence, those of the present step among them; held to 0 .. L of the call.
@@ -358,8 +358,8 @@ int rr_window_attn(const rr_shape* shape, const void* Q, const void* K, const vo
  * sets the size of the launch and of the workspace: width * page at most, the nearer to the lengths the better); Lq = the
  * positions of the step (here never 0 = L: say how many).
  * Calls that may overlap in time may share a cache that none of them writes (rr_paged_attn without RR_FLAG_ACCUMULATE only
- * reads); each needs a workspace of its own.  Pages may be shared by sequences (a common beginning) as long as nothing is
- * written to them: neither rr_paged_write nor RR_FLAG_ACCUMULATE.
+ * reads); each needs a workspace of its own.  A page may stand in several sequences' tables (a common beginning), or twice in
+ * one, as long as nothing is written to it: neither rr_paged_write nor RR_FLAG_ACCUMULATE.
  */
 typedef struct {
     void* K;
@@ -406,7 +406,9 @@ int rr_paged_attn(const rr_shape* shape, const void* Q, const rr_paged_cache* ca
  * Softmax weights that the keys get from the queries of a call, summed over the queries and over the query heads of a KV head:
  * weight[b][kv][j] = sum over heads h of the group and rows i with j <= position of i of exp(q_i k_j / sqrt(d) - lse[b][h][i]).
  *   Q, K       as for rr_dense_attn; with Lq < L the last Lq positions' queries (an observation window at a prompt's end).
- *   lse        [batch, Hq, Lq] fp32 as rr_dense_attn writes it for the same queries; rows with -inf give nothing.
+ *   lse        [batch, Hq, Lq] fp32 as rr_dense_attn, or rr_window_attn with window >= L, writes it for the same queries (for
+ *              bf16 with d = 128 the former's is off by what rounding took from its sums, 1e-4 or so; the latter's is not); rows
+ *              with -inf give nothing.
  *   weight     [batch, Hkv, L] fp32, contiguous.  Every element is written.
  *   workspace  rr_key_weights_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards; NULL where that is 0
  *              (many keys, or few queries).
