@@ -407,7 +407,7 @@ int rr_paged_attn(const rr_shape* shape, const void* Q, const rr_paged_cache* ca
  * weight[b][kv][j] = sum over heads h of the group and rows i with j <= position of i of exp(q_i k_j / sqrt(d) - lse[b][h][i]).
  *   Q, K       as for rr_dense_attn; with Lq < L the last Lq positions' queries (an observation window at a prompt's end).
  *   lse        [batch, Hq, Lq] fp32 as rr_dense_attn, or rr_window_attn with window >= L, writes it for the same queries (for
- *              bf16 with d = 128 the former's is off by what rounding took from its sums, 1e-4 or so; the latter's is not); rows
+ *              bf16 with d = 128 the former's is off by what rounding the probabilities took from its sums); rows
  *              with -inf give nothing.
  *   weight     [batch, Hkv, L] fp32, contiguous.  Every element is written.
  *   workspace  rr_key_weights_workspace_bytes() bytes, 256-byte aligned, contents undefined afterwards; NULL where that is 0
