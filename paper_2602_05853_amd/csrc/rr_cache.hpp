@@ -132,6 +132,7 @@ __device__ __forceinline__ int shares_find(const CacheArgs& c, Shares<kThreads>&
         *v = visit(c, ++b);
     }
     *base = front;
+    __syncthreads();                            // s.at may be written again
     return b;
 }
 // Blocks of the sequences in front of sequence b

@@ -63,7 +63,7 @@ k_cache_attn(CacheArgs c) {
 
     unsigned u, u_end;                                  // units (fewer than 2^31)
     Visit v;
-    int b, pair, i_lo;
+    int b, pair, i_lo, upto = 0, base = 0;
     if (c.whole) {
         // a workgroup to a sequence and pair, which stores its rows itself (their units are numbered as if all sequences visited as
         // many blocks as any may)
@@ -74,7 +74,6 @@ k_cache_attn(CacheArgs c) {
         u = blockIdx.x * (unsigned)c.whole;
         u_end = u + (unsigned)v.n;
     } else {
-        int upto, base;
         const int total = shares_scan(c, s_shares, upto);
         const Deal deal((unsigned)total * (unsigned)pairs, gridDim.x);
         if (blockIdx.x >= deal.W) return;
@@ -276,7 +275,7 @@ k_cache_attn(CacheArgs c) {
             i_lo = 0;
             if (++pair == pairs) {
                 pair = 0;
-                do v = visit(c, ++b); while (v.n == 0);  // (units are left, so a sequence that has some follows)
+                b = shares_find(c, s_shares, upto, base + v.n, &base, &v);   // (units are left; empty sequences are passed over)
             }
         }
     } while (u < u_end);
@@ -442,10 +441,7 @@ k_cache_weights(CacheArgs c, int row_tile) {
             blk = 0;
             if (++kv == c.Hkv) {
                 kv = 0;
-                do {
-                    base += v.n;
-                    v = visit(c, ++b);
-                } while (v.n == 0);
+                b = shares_find(c, s_shares, upto, base + v.n, &base, &v);
             }
         }
     }

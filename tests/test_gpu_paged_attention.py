@@ -294,3 +294,12 @@ def test_reference_of_a_row_by_hand():
     assert torch.equal(O[0, 0], V)
     ref = attend(Q[0, 0], K, V, torch.ones(1, 1, dtype=torch.bool, device=DEV))
     assert abs(float(lse) - float(ref[1])) <= float(ref[4]) + 8 * U32 * abs(float(ref[1]))
+
+
+def test_empty_sequences_between():
+    """Workgroups whose shares cross hundreds of empty sequences, in batches of one wave's lanes and of more."""
+    for batch in (60, 900):
+        lengths = [0] * batch
+        for b, n in ((0, 130), (1, 700), (batch // 2, 5), (batch - 2, 1300), (batch - 1, 257)):
+            lengths[b] = n
+        run(make(lengths, 3, 64, weight=True), 6, accumulate=True)
