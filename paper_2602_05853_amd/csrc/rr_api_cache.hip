@@ -89,6 +89,7 @@ void set_workspace(CacheArgs* c, const CachePlan& plan, void* workspace) {
     unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
     c->part_O = reinterpret_cast<float*>(ws);
     c->part_lse = c->part_O + plan.part_rows * c->d;
+    c->front = reinterpret_cast<int*>(c->part_lse + plan.part_rows);
     c->scores = plan.score_bytes ? reinterpret_cast<float*>(ws + plan.part_bytes) : nullptr;
     c->row_lse = plan.row_bytes ? reinterpret_cast<float*>(ws + plan.part_bytes + plan.score_bytes) : nullptr;
 }

@@ -135,15 +135,6 @@ __device__ __forceinline__ int shares_find(const CacheArgs& c, Shares<kThreads>&
     __syncthreads();                            // s.at may be written again
     return b;
 }
-// Blocks of the sequences in front of sequence b
-template <int kThreads>
-__device__ __forceinline__ int shares_front(const CacheArgs& c, const Shares<kThreads>& s, int upto, int b) {
-    if (c.batch <= 64) return b ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
-    const int per = (c.batch + kThreads - 1) / kThreads;
-    int front = s.pre[b / per];
-    for (int i = b / per * per; i < b; ++i) front += visit(c, i).n;
-    return front;
-}
 // How U units are dealt out to at most `workgroups`: to no more than take them in the same number of units each (fewer parts to
 // join).  All of it in 32 bits: a division of 64 takes over a hundred instructions.
 struct Deal {

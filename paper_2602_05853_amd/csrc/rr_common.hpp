@@ -227,6 +227,7 @@ struct CacheArgs {
     int row_tiles;              // a KV head's G T rows, so many at a time
     int whole;                  // 0, or blocks that a sequence visits at most: a workgroup takes all of them and there are no parts
     float* part_O; float* part_lse;   // [slot][rows of a tile][d] and [slot][rows of a tile], fp32, log2 units
+    int* front;                 // [batch] blocks of the sequences in front of each that has any, then [1] all sequences' blocks
     float* scores;              // [unit][rows of a tile][128]: products with the keys of 128 positions, -inf where masked; or nullptr
     float* row_lse;             // [batch][Hkv][G T], log2 units, +inf for a row without a key: read by the sums of the weights
 };
